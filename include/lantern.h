@@ -61,7 +61,11 @@ enum {
   LANTERN_ST_NONFINITE = 8,     /* NaN / +inf logit, or a row with no finite logit, on the walked path */
   LANTERN_ST_DEGENERATE = 16,   /* a residual without weight was met; next_token was drawn from q instead (see lantern_verify) */
   LANTERN_ST_BAD_TABLE = 32,    /* a neighbour entry outside [0, V) was met while a set A was grown (it carries no mass) */
-  LANTERN_ST_INTERNAL = 64      /* an on-chip copy did not complete within its wait limit: the sequence was not finished */
+  LANTERN_ST_INTERNAL = 64,     /* an on-chip copy did not complete within its wait limit: the sequence was not finished */
+  /* of the cache operators only */
+  LANTERN_ST_BAD_BLOCK = 128,   /* a block table entry that is needed lies outside [0, pages) */
+  LANTERN_ST_BAD_LENGTH = 256,  /* a length or count is negative, or tokens lie behind the end of the block table */
+  LANTERN_ST_BAD_PATH = 512     /* an accepted path that is not strictly increasing within [0, N), or longer than N */
 };
 
 /* Human-readable name of a return code (static storage). */
@@ -332,6 +336,129 @@ lantern_status lantern_debug_wait_test(int max_tries, int withhold_context);
  * after it, so that a benchmark can time that kernel alone with CUDA events.  Pass two NULLs
  * to switch it off.  The events are owned by the caller. */
 lantern_status lantern_verify_profile_events(void* before_fused, void* after_fused);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators around a verification step: the keys and values that the target model's forward of the drafted rows reads
+ * and writes.  (The paper's method leaves the model's forward open; these are the parts of it whose shape the drafted
+ * rows set.)  One layer's step is
+ *     lantern_rotary (queries), lantern_cache_append (keys, values), lantern_cache_attention
+ * for all N+1 rows of every sequence -- row 0 the root, row i+1 the row of node i, as in lantern_verify -- and, after
+ * lantern_verify on the logits, lantern_cache_keep with its out_accept_len and out_accept_path.
+ *
+ * Conventions, beyond those at the top of this file
+ *   - R rows per sequence (R = N+1 for drafts, 1 for plain decoding, a prompt's length for a prompt); `counts` [B] int32,
+ *     0 <= counts[b] <= R, gives the rows that a sequence really has, NULL = R for all.  Rows behind them are neither
+ *     read nor written.
+ *   - `lengths` [B] int32: tokens of the sequence in the cache BEFORE the step's rows.
+ *   - dtype LANTERN_F32 or LANTERN_BF16 is the type of rows (queries, keys, values, outputs).  Row tensors are
+ *     [B, R, heads, D] with the D components of a head side by side; the other strides are given in elements.
+ *   - `status` [B] int32, may be NULL: bits are OR-ed into it, nothing is cleared, so that one array collects the
+ *     faults of all layers of a step.
+ * ---------------------------------------------------------------------------------------- */
+
+/* A paged cache of keys and values in 8 bits, one layer.
+ *   k_code, v_code    [pages, heads, page_tokens, head_dim] e4m3 codes (3 bits of mantissa, largest value 448, no
+ *                     infinity), 16-byte aligned
+ *   k_scale, v_scale  [pages, heads] fp32: a token of page g stands for code * scale[g, head]
+ *   pages             1 <= pages; pages * heads * page_tokens <= 2^31 - 1
+ *   page_tokens       16, 32, 64 or 128
+ *   head_dim          a multiple of 16, 16 <= head_dim <= 128
+ * Token i of sequence b lies in slot i % page_tokens of page table[b, i / page_tokens]; table is [B, table_width] int32,
+ * table_width * page_tokens <= 2^30.
+ * Sequences may share pages that nothing is written to; a page that append or keep writes to belongs to one place of one
+ * sequence.  Entries of the table behind a sequence's tokens are not read. */
+typedef struct {
+  void* k_code;
+  void* v_code;
+  float* k_scale;
+  float* v_scale;
+  int32_t pages, heads, page_tokens, head_dim;
+} lantern_cache;
+
+/* Rotary positions with one to four axes (a token's index; row and column; time, height and width).
+ * Pair j (0 <= j < P, P the sum of section[0..axes-1]) turns by positions[a, b, r] * inv_freq[j], a being the axis whose
+ * section pair j falls in (section[0] pairs of axis 0, then section[1] pairs of axis 1, ...).  Pair j is the components
+ * (2j, 2j+1) if interleaved, else (j, j+P); components from 2P on stay as they are.  Angles are formed and reduced in
+ * double precision, so that far positions turn as exactly as near ones; products are fp32, rounded to dtype once.
+ *   inv_freq   [P] fp32, finite
+ *   positions  [axes, B, R] int32 */
+enum { LANTERN_MAX_AXES = 4 };
+typedef struct {
+  const float* inv_freq;
+  const int32_t* positions;
+  int32_t axes, interleaved;
+  int32_t section[LANTERN_MAX_AXES];
+} lantern_rotation;
+
+/* Rotates rows.  inverse != 0 turns by the negative angles, which is the rotation's transpose: the gradient with
+ * respect to x is lantern_rotary(gradient of out, inverse = 1).
+ *   x, out        [B, R, H, D], strides in elements (batch, row, head); out may be x itself (same strides), otherwise
+ *                 they must not overlap
+ *   B, R, H, D    B, R, H >= 0; 2 <= D <= 512, D even, 1 <= P <= D / 2, axes in [1, 4], every section >= 0 */
+lantern_status lantern_rotary(const void* x, void* out, int dtype, int B, int R, int H, int D, const int64_t x_stride[3],
+                              const int64_t out_stride[3], const lantern_rotation* rotation, int inverse,
+                              void* cuda_stream);
+
+/* Appends rows to the cache: row r of sequence b becomes token lengths[b] + r.  Keys are rotated on the way if
+ * `rotation` is given (NULL: stored as they come); nothing is rounded in between.
+ *
+ * A scale is a power of two, 2^e with -100 <= e: the least one under which no value of the rows that come into the
+ * block exceeds 448, except that a block that already holds tokens of the sequence keeps its scale if that is larger.
+ * If its scale grows, the tokens that it holds are coded anew (an exact change but for values that fall below the
+ * smallest normal code).  Appending at slot 0 starts a block afresh.  Codes round to nearest even.
+ * A NaN or infinite value is stored as the NaN code, sets LANTERN_ST_NONFINITE and does not count for the scale.
+ * With LANTERN_ST_BAD_LENGTH nothing of the sequence is written, with LANTERN_ST_BAD_BLOCK nothing of the block.
+ *
+ *   k, v          [B, R, heads, D], strides in elements (batch, row, head); heads and D are the cache's */
+lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int B, int R, const int64_t k_stride[3],
+                                    const int64_t v_stride[3], const lantern_cache* cache, const int32_t* table,
+                                    int table_width, const int32_t* lengths, const int32_t* counts,
+                                    const lantern_rotation* rotation, int32_t* status, void* cuda_stream);
+
+/* Attention of the step's rows to the cache, after lantern_cache_append has put their keys and values there.
+ *     out[b, r, h] = sum_c softmax_c(scale * q[b, r, h] . k_c) v_c,    k_c, v_c of cache head h / (q_heads / heads),
+ * over the tokens c that row r sees: starts[b] <= c, and c < lengths[b], or c = lengths[b] + j where j is r itself or an
+ * ancestor of r (tree_parents as in lantern_verify: node i is row i+1, the root row 0 is everyone's ancestor; NULL =
+ * chain: j <= r).  A row that sees nothing gives zeros.  A NaN code makes the rows that see it NaN, at least in the
+ * components concerned, and no other row.  A sequence with a fault (BAD_LENGTH, BAD_BLOCK, BAD_PARENT among its rows)
+ * gives NaN in rows that the fault concerns.
+ *
+ * Scores, the softmax's maximum and sum and the outputs are fp32; queries enter the products exactly with bf16 and to 22
+ * bits with fp32, probabilities to 11 bits with bf16 (half a bit of which the output's own 8 bits show) and to 22 with fp32.
+ *
+ *   q             [B, R, q_heads, D], strides in elements; 16-byte aligned rows are fastest, any alignment is served
+ *   out           [B, R, q_heads, D] contiguous, dtype of q
+ *   q_heads       a multiple of the cache's heads
+ *   tree_parents  [B, R-1] int32, R <= 1025; NULL = chain, any R
+ *   starts        [B] int32, NULL = 0 (tokens ahead of starts[b] are padding and are not read)
+ *   scale         finite
+ *   workspace     lantern_cache_attention_workspace_bytes(...) bytes, 256-byte aligned; NULL if that is 0 */
+size_t lantern_cache_attention_workspace_bytes(int dtype, int B, int R, int q_heads, const lantern_cache* cache,
+                                               int table_width);
+
+lantern_status lantern_cache_attention(const void* q, void* out, int dtype, int B, int R, int q_heads,
+                                       const int64_t q_stride[3], const lantern_cache* cache, const int32_t* table,
+                                       int table_width, const int32_t* lengths, const int32_t* counts,
+                                       const int32_t* starts, const int32_t* tree_parents, float scale, int32_t* status,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Keeps the accepted path's tokens after lantern_verify: with n = accept_len[b], token lengths[b] + 1 + j becomes what
+ * token lengths[b] + 1 + accept_path[b, j] was, j < n (the root's token at lengths[b] stays where it is), and
+ * out_lengths[b] = lengths[b] + 1 + n.  Tokens behind are undefined.  Where a token moves into a block of a smaller
+ * scale, that block takes the larger one and its tokens are coded anew.
+ * A fault (BAD_PATH, BAD_LENGTH, BAD_BLOCK) leaves the sequence as it is, with out_lengths[b] = lengths[b].
+ *   accept_len    [B], accept_path [B, N] as lantern_verify writes them; 0 <= N <= 1024
+ *   out_lengths   [B], must not overlap lengths */
+lantern_status lantern_cache_keep(const lantern_cache* cache, const int32_t* table, int table_width,
+                                  const int32_t* lengths, const int32_t* accept_len, const int32_t* accept_path, int B,
+                                  int N, int32_t* out_lengths, int32_t* status, void* cuda_stream);
+
+/* Reads tokens first[b] .. first[b] + counts[b] - 1 back (counts NULL: R of them).
+ *   out_k, out_v  [B, R, heads, D] contiguous, dtype; 16-byte aligned.  With a fault (BAD_LENGTH: any of the tokens lies
+ *                 outside the table; BAD_BLOCK) the rows concerned are NaN */
+lantern_status lantern_cache_read(const lantern_cache* cache, const int32_t* table, int table_width,
+                                  const int32_t* first, const int32_t* counts, int B, int R, int dtype, void* out_k,
+                                  void* out_v, int32_t* status, void* cuda_stream);
 
 #ifdef __cplusplus
 }

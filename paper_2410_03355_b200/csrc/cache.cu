@@ -1,0 +1,514 @@
+// The paged 8-bit cache of keys and values: appending rows (keys rotated on the way), keeping an accepted path, reading back.
+//
+// A block (page, head) has one scale for its keys and one for its values.  Scales are powers of two, so that taking a larger one moves the
+// codes' exponents and loses nothing but bits that fall below the smallest normal code.
+#include "cache_common.cuh"
+
+namespace lantern {
+
+struct CacheView {
+  uint8_t* code[2];    // keys, values
+  float* scale[2];
+  const int32_t* table;
+  int pages, heads, S, D, width;
+  __device__ __forceinline__ int64_t block(int page, int head) const { return static_cast<int64_t>(page) * heads + head; }
+  __device__ __forceinline__ uint8_t* row(int which, int page, int head, int slot) const {
+    return code[which] + ((block(page, head) * S) + slot) * D;
+  }
+};
+static CacheView view_of(const lantern_cache* c, const int32_t* table, int width) {
+  return {{static_cast<uint8_t*>(c->k_code), static_cast<uint8_t*>(c->v_code)}, {c->k_scale, c->v_scale}, table,
+          c->pages, c->heads, c->page_tokens, c->head_dim, width};
+}
+
+__device__ __forceinline__ uint2 recode8(uint2 codes, float ratio) {   // codes * ratio, ratio <= 1
+  float a[4], b[4];
+  decode4(codes.x, a), decode4(codes.y, b);
+  return make_uint2(encode4(a[0] * ratio, a[1] * ratio, a[2] * ratio, a[3] * ratio), encode4(b[0] * ratio, b[1] * ratio, b[2] * ratio, b[3] * ratio));
+}
+
+// ---- append -------------------------------------------------------------------------------------------------------------
+
+struct AppendParams {
+  CacheView c;
+  const void* x[2];
+  RowStride xs[2];
+  Rotation rot;
+  const int32_t* lengths;
+  const int32_t* counts;
+  int32_t* status;
+  int B, R;
+  int vec;             // rows may be read eight components at a time
+  int heads_per_cta;
+};
+
+// What of block j (the j-th that the sequence's rows touch) is new: slots [low, high), the first of them row `row`; held slots ahead of them.
+struct Span {
+  int page, low, high, row, fault;
+};
+__device__ __forceinline__ Span append_span(const AppendParams& P, int b, int j) {
+  Span s{0, 0, 0, 0, 0};
+  const int len = __ldg(P.lengths + b), n = P.counts ? __ldg(P.counts + b) : P.R;
+  if (len < 0 || n < 0 || n > P.R || static_cast<int64_t>(len) + n > static_cast<int64_t>(P.c.width) * P.c.S) {
+    s.fault = LANTERN_ST_BAD_LENGTH;
+    return s;
+  }
+  const int S = P.c.S, block = len / S + j;
+  const int64_t first = static_cast<int64_t>(block) * S;
+  if (first >= static_cast<int64_t>(len) + n) return s;   // (nothing: low == high)
+  const int page = __ldg(P.c.table + static_cast<int64_t>(b) * P.c.width + block);
+  if (page < 0 || page >= P.c.pages) {
+    s.fault = LANTERN_ST_BAD_BLOCK;
+    return s;
+  }
+  s.page = page;
+  s.low = j == 0 ? len - static_cast<int>(first) : 0;
+  const int64_t left = static_cast<int64_t>(len) + n - first;
+  s.high = left < S ? static_cast<int>(left) : S;
+  s.row = j == 0 ? 0 : static_cast<int>(first - len);
+  return s;
+}
+
+// Components [d, d + 8) of a row of keys (turned) or values.  table: cosines and sines of the row's pairs, NULL = not rotated.
+template <bool BF16>
+__device__ __forceinline__ void new_values(const AppendParams& P, const typename Row<BF16>::T* p, int d, const float2* table, float (&v)[8]) {
+  if (P.vec) {
+    Row<BF16>::get8(p + d, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = Row<BF16>::get(p + d + i);
+  }
+  if (!table) return;
+  const int pairs = P.rot.pairs;
+  if (d >= 2 * pairs) return;
+  if (P.rot.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      if (d + i < 2 * pairs) {
+        const float2 w = table[(d + i) >> 1];
+        const float a = v[i], b = v[i + 1];
+        v[i] = turned_low(a, b, w);
+        v[i + 1] = turned_high(a, b, w);
+      }
+    }
+  } else if (P.vec && pairs % 8 == 0) {   // the eight lie in one half, their partners in the other
+    float o[8];
+    const bool lower = d < pairs;
+    const int j = lower ? d : d - pairs;
+    Row<BF16>::get8(p + (lower ? d + pairs : d - pairs), o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 w = table[j + i];
+      v[i] = lower ? turned_low(v[i], o[i], w) : turned_high(o[i], v[i], w);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (d + i < 2 * pairs) {
+        const bool lower = d + i < pairs;
+        const int j = lower ? d + i : d + i - pairs;
+        const float2 w = table[j];
+        const float o = Row<BF16>::get(p + (lower ? d + i + pairs : j));
+        v[i] = lower ? turned_low(v[i], o, w) : turned_high(o, v[i], w);
+      }
+    }
+  }
+}
+// largest finite magnitude; `odd` is set if one of them is not finite, which then becomes NaN
+__device__ __forceinline__ float magnitude(float (&v)[8], int& odd) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (fabsf(v[i]) < __int_as_float(0x7f800000)) {
+      m = fmaxf(m, fabsf(v[i]));
+    } else {
+      odd = 1;
+      v[i] = __int_as_float(0x7fffffff);
+    }
+  }
+  return m;
+}
+// the scale that the block gets
+__device__ __forceinline__ float new_scale(float amax, float old, bool held, int& odd) {
+  const float need = scale_for(amax);
+  if (!held) return need;
+  if (!usable_scale(old)) {
+    odd = 1;
+    return need;
+  }
+  return fmaxf(need, old);
+}
+
+// A CTA per touched block and run of heads: the block's angles are formed once, then every head's keys and values go through registers, U units of
+// eight components per thread: maximum over the block, scale, codes.  Bound by HBM.
+constexpr int AT = 256;
+template <bool BF16, int U>
+__global__ void __launch_bounds__(AT) lantern_append_kernel(AppendParams P) {
+  using T = typename Row<BF16>::T;
+  extern __shared__ float2 angles[];   // [new slots][pairs]
+  __shared__ float most[2][AT / 32];
+  const int b = blockIdx.z, j = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int h0 = blockIdx.x * P.heads_per_cta, h1 = min(h0 + P.heads_per_cta, P.c.heads);
+  const Span s = append_span(P, b, j);
+  if (s.fault && tid == 0 && P.status) atomicOr(P.status + b, s.fault);
+  const int n = s.high - s.low;
+  if (s.fault || n <= 0) return;
+  const bool rotate = P.rot.inv_freq != nullptr;
+  const int pairs = rotate ? P.rot.pairs : 1;
+  if (rotate)
+    for (int i = tid; i < n * pairs; i += AT) angles[i] = turn(P.rot, static_cast<int64_t>(b) * P.R + s.row + i / pairs, i % pairs);
+  const int D = P.c.D, per_row = D >> 3, units = n * per_row;
+  int odd = 0, turn_of = 0;
+  for (int h = h0; h < h1; ++h) {
+    for (int which = 0; which < 2; ++which) {
+      const T* x = static_cast<const T*>(P.x[which]) + b * P.xs[which].b + h * P.xs[which].h;
+      float v[U][8], m = 0.0f;
+      if (turn_of == 0) __syncthreads();   // the angles are there
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = tid + u * AT;
+        if (i < units) {
+          const int t = i / per_row;
+          new_values<BF16>(P, x + (s.row + t) * P.xs[which].r, (i - t * per_row) * 8, rotate && which == 0 ? angles + t * pairs : nullptr, v[u]);
+          m = fmaxf(m, magnitude(v[u], odd));
+        }
+      }
+      m = warp_max(m);
+      float* mine = most[turn_of & 1];
+      if (lane == 0) mine[warp] = m;
+      const int64_t block = P.c.block(s.page, h);
+      const float old = P.c.scale[which][block];
+      __syncthreads();   // (also: everybody has read the scale; the other buffer's readers are through)
+#pragma unroll
+      for (int w = 0; w < AT / 32; ++w) m = fmaxf(m, mine[w]);
+      const float scale = new_scale(m, old, s.low > 0, odd);
+      const Divider over = divider(scale);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = tid + u * AT;
+        if (i < units) {
+          const int t = i / per_row;
+          const uint2 c = make_uint2(encode4(over(v[u][0]), over(v[u][1]), over(v[u][2]), over(v[u][3])),
+                                     encode4(over(v[u][4]), over(v[u][5]), over(v[u][6]), over(v[u][7])));
+          *reinterpret_cast<uint2*>(P.c.row(which, s.page, h, s.low + t) + (i - t * per_row) * 8) = c;
+        }
+      }
+      if (s.low > 0 && scale != old) {   // what the block holds is coded anew
+        const float ratio = usable_scale(old) ? old / scale : 0.0f;
+        uint2* held = reinterpret_cast<uint2*>(P.c.row(which, s.page, h, 0));
+        for (int i = tid; i < s.low * per_row; i += AT) held[i] = recode8(held[i], ratio);
+      }
+      if (tid == 0 && scale != old) P.c.scale[which][block] = scale;
+      ++turn_of;
+    }
+  }
+  if (odd && P.status) atomicOr(P.status + b, LANTERN_ST_NONFINITE);
+}
+
+// Few rows a sequence: a warp per touched block, head and kind.  The rows are read twice (the second time from L1); angles are formed by the
+// lane that needs them.  Bound by latency.
+constexpr int FT = 128;
+template <bool BF16>
+__global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) {
+  using T = typename Row<BF16>::T;
+  __shared__ float2 angles[FT / 32][kMaxHeadDim / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int item = blockIdx.x * (FT / 32) + warp;   // (head, kind)
+  const int b = blockIdx.z, j = blockIdx.y;
+  if (item >= 2 * P.c.heads) return;
+  const int which = item & 1, h = item >> 1;
+  const Span s = append_span(P, b, j);
+  if (s.fault && item == 0 && lane == 0 && P.status) atomicOr(P.status + b, s.fault);
+  const int n = s.high - s.low;
+  if (s.fault || n <= 0) return;
+  const int D = P.c.D, per_row = D >> 3;
+  const bool rotate = P.rot.inv_freq != nullptr && which == 0;
+  const T* x = static_cast<const T*>(P.x[which]) + b * P.xs[which].b + h * P.xs[which].h;
+  const int64_t block = P.c.block(s.page, h);
+  const float old = P.c.scale[which][block];
+  int odd = 0;
+  float m = 0.0f, v[8];
+  auto values = [&](int t) {   // row t's eight components of this lane (per_row <= 16 lanes take part)
+    const T* p = x + (s.row + t) * P.xs[which].r;
+    if (rotate) {
+      __syncwarp();
+      for (int i = lane; i < P.rot.pairs; i += 32) angles[warp][i] = turn(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, i);
+      __syncwarp();
+    }
+    if (lane < per_row) new_values<BF16>(P, p, lane * 8, rotate ? angles[warp] : nullptr, v);
+    return lane < per_row ? magnitude(v, odd) : 0.0f;
+  };
+  for (int t = 0; t < n; ++t) m = fmaxf(m, values(t));
+  m = warp_max(m);
+  const float scale = new_scale(m, old, s.low > 0, odd);
+  const Divider over = divider(scale);
+  for (int t = n - 1; t >= 0; --t) {
+    if (t != n - 1) values(t);   // (the last row's are still there)
+    if (lane < per_row)
+      *reinterpret_cast<uint2*>(P.c.row(which, s.page, h, s.low + t) + lane * 8) =
+          make_uint2(encode4(over(v[0]), over(v[1]), over(v[2]), over(v[3])), encode4(over(v[4]), over(v[5]), over(v[6]), over(v[7])));
+  }
+  if (s.low > 0 && scale != old) {
+    const float ratio = usable_scale(old) ? old / scale : 0.0f;
+    uint2* held = reinterpret_cast<uint2*>(P.c.row(which, s.page, h, 0));
+    for (int i = lane; i < s.low * per_row; i += 32) held[i] = recode8(held[i], ratio);
+  }
+  if (lane == 0 && scale != old) P.c.scale[which][block] = scale;
+  if (odd && P.status) atomicOr(P.status + b, LANTERN_ST_NONFINITE);
+}
+
+template <bool BF16, int U>
+static cudaError_t launch_append(const AppendParams& P, dim3 grid, size_t smem, cudaStream_t st) {
+  static DeviceFlags ready;
+  const cudaError_t e = allow_shared_memory(lantern_append_kernel<BF16, U>, 128 * (kMaxHeadDim / 2) * sizeof(float2), ready);
+  if (e != cudaSuccess) return e;
+  lantern_append_kernel<BF16, U><<<grid, AT, smem, st>>>(P);
+  return cudaGetLastError();
+}
+
+// ---- keep ---------------------------------------------------------------------------------------------------------------
+
+struct KeepParams {
+  CacheView c;
+  const int32_t* lengths;
+  const int32_t* accept_len;
+  const int32_t* path;
+  int32_t* out_lengths;
+  int32_t* status;
+  int N;
+};
+
+// A warp per sequence, head and kind.  Targets ascend and no target lies behind its source (a path is increasing), so that going through the
+// targets in order, block by block, never overwrites a source that is still needed.  Bound by latency.
+constexpr int KT = 128;
+__global__ void __launch_bounds__(KT) lantern_keep_kernel(KeepParams P) {
+  const int lane = threadIdx.x & 31;
+  const int item = blockIdx.x * (KT / 32) + (threadIdx.x >> 5), b = blockIdx.y;
+  if (item >= 2 * P.c.heads) return;
+  const int which = item & 1, h = item >> 1, S = P.c.S, D = P.c.D, N = P.N;
+  const int32_t* path = P.path + static_cast<int64_t>(b) * N;
+  const int32_t* table = P.c.table + static_cast<int64_t>(b) * P.c.width;
+  const int len = __ldg(P.lengths + b), n = __ldg(P.accept_len + b);
+  int fault = 0, moved = 0;   // moved: some token of the path moves
+  if (len < 0) fault |= LANTERN_ST_BAD_LENGTH;
+  if (n < 0 || n > N) fault |= LANTERN_ST_BAD_PATH;
+  if (!fault) {
+    const int64_t room = static_cast<int64_t>(P.c.width) * S;
+    if (static_cast<int64_t>(len) + 1 + n > room) fault |= LANTERN_ST_BAD_LENGTH;
+    for (int i = lane; i < n; i += 32) {
+      const int at = __ldg(path + i), before = i ? __ldg(path + i - 1) : -1;
+      if (at <= before || at < 0 || at >= N) {
+        fault |= LANTERN_ST_BAD_PATH;
+      } else if (at != i) {
+        moved = 1;
+        const int64_t from = static_cast<int64_t>(len) + 1 + at, to = static_cast<int64_t>(len) + 1 + i;
+        if (from >= room || to >= room) {
+          fault |= LANTERN_ST_BAD_LENGTH;
+        } else if (static_cast<unsigned>(__ldg(table + from / S)) >= static_cast<unsigned>(P.c.pages) ||
+                   static_cast<unsigned>(__ldg(table + to / S)) >= static_cast<unsigned>(P.c.pages)) {
+          fault |= LANTERN_ST_BAD_BLOCK;
+        }
+      }
+    }
+  }
+  fault = __reduce_or_sync(kFull, fault);
+  moved = __any_sync(kFull, moved);
+  if (item == 0 && lane == 0) {
+    P.out_lengths[b] = fault ? len : len + 1 + n;
+    if (fault && P.status) atomicOr(P.status + b, fault);
+  }
+  if (fault || !moved) return;
+  const int first = len + 1, vecs = D >> 4;   // 16 bytes of a row per lane, 32 / vecs rows at a time
+  const int rows = 32 / vecs, sub = lane / vecs, at = lane - sub * vecs;
+  for (int j0 = 0; j0 < n;) {   // targets [j0, j1) of one block
+    const int block = (first + j0) / S, j1 = min(n, (block + 1) * S - first);
+    const int page = __ldg(table + block);
+    float* own = P.c.scale[which] + P.c.block(page, h);
+    float most = 0.0f;
+    int moves = 0;
+    for (int j = j0 + lane; j < j1; j += 32) {
+      const int from = __ldg(path + j);
+      moves |= from != j;
+      if (from != j) most = fmaxf(most, P.c.scale[which][P.c.block(__ldg(table + (first + from) / S), h)]);
+    }
+    most = warp_max(most);
+    if (__any_sync(kFull, moves)) {
+      const float old = *own, scale = fmaxf(old, most);
+      __syncwarp();
+      if (scale != old) {
+        const float ratio = old / scale;
+        uint2* held = reinterpret_cast<uint2*>(P.c.row(which, page, h, 0));
+        for (int i = lane; i < S * D / 8; i += 32) held[i] = recode8(held[i], ratio);
+        if (lane == 0) *own = scale;
+        __syncwarp();
+      }
+      for (int j = j0; j < j1; j += rows) {
+        const int mine = j + sub;
+        const int from = sub < rows && mine < j1 ? __ldg(path + mine) : mine;
+        uint4 c = make_uint4(0, 0, 0, 0);
+        if (from != mine) {
+          const int token = first + from, source = __ldg(table + token / S);
+          c = *reinterpret_cast<const uint4*>(P.c.row(which, source, h, token % S) + at * 16);
+          const float theirs = source == page ? scale : P.c.scale[which][P.c.block(source, h)];
+          if (theirs != scale) {
+            const float ratio = theirs / scale;
+            const uint2 lo = recode8(make_uint2(c.x, c.y), ratio), hi = recode8(make_uint2(c.z, c.w), ratio);
+            c = make_uint4(lo.x, lo.y, hi.x, hi.y);
+          }
+        }
+        __syncwarp();   // the sources of these rows are read before a row is written
+        if (from != mine) *reinterpret_cast<uint4*>(P.c.row(which, page, h, (first + mine) % S) + at * 16) = c;
+        __syncwarp();
+      }
+    }
+    j0 = j1;
+  }
+}
+
+// ---- read ---------------------------------------------------------------------------------------------------------------
+
+struct ReadParams {
+  CacheView c;
+  const int32_t* first;
+  const int32_t* counts;
+  int32_t* status;
+  void* out[2];
+  int R;
+  int64_t units;   // B * R * heads * D / 16
+};
+
+// A thread per 16 components of a row, keys and values.  Bound by HBM: one byte in, two or four out.
+constexpr int DT = 256;
+template <bool BF16>
+__global__ void __launch_bounds__(DT) lantern_read_kernel(ReadParams P) {
+  using T = typename Row<BF16>::T;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * DT + threadIdx.x;
+  if (i >= P.units) return;
+  const int vecs = P.c.D >> 4, per_row = P.c.heads * vecs;
+  const int64_t row = i / per_row;
+  const int rest = static_cast<int>(i - row * per_row), h = rest / vecs, d = (rest - h * vecs) * 16;
+  const int b = static_cast<int>(row / P.R), r = static_cast<int>(row - static_cast<int64_t>(b) * P.R);
+  const int first = __ldg(P.first + b), n = P.counts ? __ldg(P.counts + b) : P.R;
+  int fault = 0, page = 0;
+  const int64_t token = static_cast<int64_t>(first) + r;
+  if (first < 0 || n < 0 || n > P.R || static_cast<int64_t>(first) + n > static_cast<int64_t>(P.c.width) * P.c.S) {
+    fault = LANTERN_ST_BAD_LENGTH;
+  } else if (r >= n) {
+    return;
+  } else {
+    page = __ldg(P.c.table + static_cast<int64_t>(b) * P.c.width + token / P.c.S);
+    if (page < 0 || page >= P.c.pages) fault = LANTERN_ST_BAD_BLOCK;
+  }
+  if (fault && rest == 0 && P.status) atomicOr(P.status + b, fault);
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float v[16];
+    if (fault) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = __int_as_float(0x7fffffff);
+    } else {
+      const uint4 c = *reinterpret_cast<const uint4*>(P.c.row(which, page, h, static_cast<int>(token % P.c.S)) + d);
+      const float scale = P.c.scale[which][P.c.block(page, h)];
+      const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float x[4];
+        decode4(w[q], x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e] * scale;
+      }
+    }
+    T* out = static_cast<T*>(P.out[which]) + i * 16;
+    const float lo[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, hi[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
+    Row<BF16>::put8(out, lo);
+    Row<BF16>::put8(out + 8, hi);
+  }
+}
+
+}  // namespace lantern
+
+using namespace lantern;
+
+extern "C" lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int B, int R, const int64_t k_stride[3],
+                                               const int64_t v_stride[3], const lantern_cache* cache, const int32_t* table, int table_width,
+                                               const int32_t* lengths, const int32_t* counts, const lantern_rotation* rotation, int32_t* status,
+                                               void* cuda_stream) {
+  if (dtype != LANTERN_F32 && dtype != LANTERN_BF16) return LANTERN_E_PARAM;
+  lantern_status bad = check_cache(cache, table, table_width, B);
+  if (bad != LANTERN_OK) return bad;
+  if (B < 0 || B > 65535 || R < 0) return LANTERN_E_SHAPE;
+  AppendParams P;
+  P.rot.inv_freq = nullptr;
+  if (rotation && (bad = make_rotation(rotation, B, R, cache->head_dim, &P.rot)) != LANTERN_OK) return bad;
+  if (B == 0 || R == 0) return LANTERN_OK;
+  if (!k || !v || !k_stride || !v_stride || !lengths) return LANTERN_E_NULL;
+  const int S = cache->page_tokens, D = cache->head_dim, H = cache->heads, size = dtype == LANTERN_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(k) % size || reinterpret_cast<uintptr_t>(v) % size) return LANTERN_E_ALIGN;
+  const int64_t touched = R == 1 ? 1 : (static_cast<int64_t>(R) + S - 2) / S + 1;   // blocks that R rows can touch
+  if (touched > 65535) return LANTERN_E_SHAPE;
+  P.c = view_of(cache, table, table_width);
+  P.x[0] = k;
+  P.x[1] = v;
+  P.xs[0] = {k_stride[0], k_stride[1], k_stride[2]};
+  P.xs[1] = {v_stride[0], v_stride[1], v_stride[2]};
+  P.lengths = lengths;
+  P.counts = counts;
+  P.status = status;
+  P.B = B;
+  P.R = R;
+  const int64_t ks[3] = {k_stride[0], k_stride[1], k_stride[2]}, vs[3] = {v_stride[0], v_stride[1], v_stride[2]};
+  P.vec = aligned16(k, ks, size) && aligned16(v, vs, size);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool bf = dtype == LANTERN_BF16;
+  cudaError_t e;
+  if (R <= 4) {
+    const dim3 grid((2 * H + FT / 32 - 1) / (FT / 32), static_cast<unsigned>(touched), B);
+    if (bf) lantern_append_few_kernel<true><<<grid, FT, 0, st>>>(P);
+    else lantern_append_few_kernel<false><<<grid, FT, 0, st>>>(P);
+    e = cudaGetLastError();
+  } else {
+    P.heads_per_cta = H < 4 ? H : 4;
+    const dim3 grid((H + P.heads_per_cta - 1) / P.heads_per_cta, static_cast<unsigned>(touched), B);
+    const size_t smem = rotation ? static_cast<size_t>(S) * P.rot.pairs * sizeof(float2) : 0;
+    const int u = (S * D / 8 + AT - 1) / AT;
+    if (u <= 1) e = bf ? launch_append<true, 1>(P, grid, smem, st) : launch_append<false, 1>(P, grid, smem, st);
+    else if (u <= 2) e = bf ? launch_append<true, 2>(P, grid, smem, st) : launch_append<false, 2>(P, grid, smem, st);
+    else if (u <= 4) e = bf ? launch_append<true, 4>(P, grid, smem, st) : launch_append<false, 4>(P, grid, smem, st);
+    else e = bf ? launch_append<true, 8>(P, grid, smem, st) : launch_append<false, 8>(P, grid, smem, st);
+  }
+  return e == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
+}
+
+extern "C" lantern_status lantern_cache_keep(const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths,
+                                             const int32_t* accept_len, const int32_t* accept_path, int B, int N, int32_t* out_lengths,
+                                             int32_t* status, void* cuda_stream) {
+  const lantern_status bad = check_cache(cache, table, table_width, B);
+  if (bad != LANTERN_OK) return bad;
+  if (B < 0 || B > 65535 || N < 0 || N > 1024) return LANTERN_E_SHAPE;
+  if (B == 0) return LANTERN_OK;
+  if (!lengths || !accept_len || !out_lengths || (N > 0 && !accept_path)) return LANTERN_E_NULL;
+  KeepParams P{view_of(cache, table, table_width), lengths, accept_len, accept_path, out_lengths, status, N};
+  const dim3 grid((2 * cache->heads + KT / 32 - 1) / (KT / 32), B);
+  lantern_keep_kernel<<<grid, KT, 0, static_cast<cudaStream_t>(cuda_stream)>>>(P);
+  return cudaGetLastError() == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
+}
+
+extern "C" lantern_status lantern_cache_read(const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* first,
+                                             const int32_t* counts, int B, int R, int dtype, void* out_k, void* out_v, int32_t* status,
+                                             void* cuda_stream) {
+  if (dtype != LANTERN_F32 && dtype != LANTERN_BF16) return LANTERN_E_PARAM;
+  const lantern_status bad = check_cache(cache, table, table_width, B);
+  if (bad != LANTERN_OK) return bad;
+  if (B < 0 || R < 0 || static_cast<int64_t>(B) * R > INT32_MAX) return LANTERN_E_SHAPE;
+  if (B == 0 || R == 0) return LANTERN_OK;
+  if (!first || !out_k || !out_v) return LANTERN_E_NULL;
+  if ((reinterpret_cast<uintptr_t>(out_k) & 15) || (reinterpret_cast<uintptr_t>(out_v) & 15)) return LANTERN_E_ALIGN;
+  ReadParams P{view_of(cache, table, table_width), first, counts, status, {out_k, out_v}, R,
+               static_cast<int64_t>(B) * R * cache->heads * (cache->head_dim / 16)};
+  const int64_t grid = (P.units + DT - 1) / DT;
+  if (grid > INT32_MAX) return LANTERN_E_SHAPE;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (dtype == LANTERN_BF16) lantern_read_kernel<true><<<static_cast<unsigned>(grid), DT, 0, st>>>(P);
+  else lantern_read_kernel<false><<<static_cast<unsigned>(grid), DT, 0, st>>>(P);
+  return cudaGetLastError() == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
+}

@@ -1,0 +1,137 @@
+// What the attention kernels share: the call's parameters, what a unit of work covers, tensor maps of the codes, and the joining of parts.
+#pragma once
+
+#include <cuda.h>
+
+#include "cache_common.cuh"
+
+namespace lantern {
+
+constexpr int kTileTokens = 64;   // tokens per step of the long axis
+
+struct AttendParams {
+  const void* q;
+  void* out;
+  RowStride qs;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* counts;
+  const int32_t* starts;
+  const int32_t* parents;
+  int32_t* status;
+  float* parts;       // [unit][split][rows of a unit][DP] numerators, relative to 2^maximum
+  float2* part_ml;    // [unit][split][rows of a unit] maximum (base 2), sum
+  int B, R, q_heads, heads, G, S, D, width, pages;
+  int row_tiles;      // units per sequence and cache head
+  int splits;         // parts that a unit's tokens are divided into, at most
+  int least;          // tiles per part, at least
+  int vec;            // query rows may be read 16 bytes at a time
+  float scale_log2;   // scale * log2(e)
+};
+
+// What rows [m0, m0 + ROWS) of one sequence and cache head (row m: step row m / G, head m % G) have to read.
+struct Unit {
+  int b, h, m0, split;
+  int len, n;            // cached tokens, rows of the step (what the checks leave of them)
+  int begin, end;        // tokens [begin, end) that some row of the unit may see
+  int tile0, lo, hi;     // first tile of the unit; tiles [lo, hi) of it are this part's
+  int parts;             // parts with work
+  int fault;
+  bool rows;             // there are rows to answer
+};
+template <int ROWS>
+__device__ __forceinline__ Unit unit_of(const AttendParams& P, int64_t unit, int split) {
+  Unit u;
+  u.split = split;
+  const int mt = static_cast<int>(unit % P.row_tiles);
+  const int64_t bh = unit / P.row_tiles;
+  u.b = static_cast<int>(bh / P.heads);
+  u.h = static_cast<int>(bh - static_cast<int64_t>(u.b) * P.heads);
+  u.m0 = mt * ROWS;
+  u.len = __ldg(P.lengths + u.b);
+  u.n = P.counts ? __ldg(P.counts + u.b) : P.R;
+  u.begin = P.starts ? max(__ldg(P.starts + u.b), 0) : 0;
+  u.fault = 0;
+  if (u.len < 0 || u.n < 0 || u.n > P.R || static_cast<int64_t>(u.len) + u.n > static_cast<int64_t>(P.width) * P.S) {
+    u.fault = LANTERN_ST_BAD_LENGTH;
+    if (u.n < 0 || u.n > P.R) u.n = P.R;
+    u.len = 0;
+  }
+  const int first = u.m0 / P.G, last = min(u.n - 1, (u.m0 + ROWS - 1) / P.G);
+  u.rows = first < u.n;
+  u.end = u.fault ? u.begin : u.len + last + 1;   // (an ancestor has a smaller row: trees and chains alike)
+  u.tile0 = u.begin / kTileTokens;
+  const int tiles = u.end > u.begin ? (u.end + kTileTokens - 1) / kTileTokens - u.tile0 : 0;
+  const int per = max((tiles + P.splits - 1) / P.splits, P.least);
+  u.parts = max(1, (tiles + per - 1) / per);
+  u.lo = split * per;
+  u.hi = min(tiles, u.lo + per);
+  return u;
+}
+
+// Which of the step's rows a row sees, as bits [rows of the unit][words]; false if a parent is out of range.  All threads of the CTA; `nodes` holds R - 1 words.
+__device__ __forceinline__ void ancestor_bits(const AttendParams& P, const Unit& u, int rows, int words, int32_t* nodes, uint32_t* bits, int* fault,
+                                              int tid, int threads) {
+  const int first = u.m0 / P.G;
+  const int32_t* parents = P.parents + static_cast<int64_t>(u.b) * (P.R - 1);
+  for (int i = tid; i < u.n - 1; i += threads) {
+    const int p = __ldg(parents + i);
+    nodes[i] = p;
+    if (p < -1 || p >= i) atomicOr(fault, LANTERN_ST_BAD_PARENT);
+  }
+  for (int i = tid; i < rows * words; i += threads) bits[i] = 0;
+  __syncthreads();
+  if (*fault) return;
+  for (int i = tid; i < rows; i += threads) {
+    int r = first + i;
+    if (r >= u.n) break;
+    uint32_t* mine = bits + i * words;
+    for (; r > 0; r = nodes[r - 1] + 1) mine[r >> 5] |= 1u << (r & 31);
+    mine[0] |= 1u;
+  }
+}
+
+// Joins the parts of a unit: a CTA per unit, a thread per four components.
+template <int ROWS, int DP, bool BF16>
+__global__ void __launch_bounds__(128) lantern_join_kernel(AttendParams P) {
+  using T = typename Row<BF16>::T;
+  grid_dependency_wait();
+  const Unit u = unit_of<ROWS>(P, blockIdx.x, 0);
+  if (!u.rows || u.parts == 1) return;
+  const int rows = min(ROWS, u.n * P.G - u.m0), per_row = P.D >> 2;
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * P.splits;
+  for (int i = threadIdx.x; i < rows * per_row; i += 128) {
+    const int row = i / per_row, d = (i - row * per_row) * 4;
+    float M = -INFINITY;
+    for (int s = 0; s < u.parts; ++s) M = fmaxf(M, P.part_ml[(base + s) * ROWS + row].x);
+    const float sub = M == -INFINITY ? 0.0f : M;
+    float L = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s = 0; s < u.parts; ++s) {
+      const float2 ml = P.part_ml[(base + s) * ROWS + row];
+      const float w = ex2_approx(ml.x - sub);
+      const float4 o = *reinterpret_cast<const float4*>(P.parts + ((base + s) * ROWS + row) * DP + d);
+      L += ml.y * w;
+      acc.x += o.x * w, acc.y += o.y * w, acc.z += o.z * w, acc.w += o.w * w;
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;   // (nothing seen: zeros; NaN stays)
+    const int m = u.m0 + row, r = m / P.G;
+    T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (m - r * P.G)) * P.D + d;
+    const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+    if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(bf16x2_round(v[0], v[1]), bf16x2_round(v[2], v[3]));
+    else *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int row, int page, uint64_t* bar) {   // x = 0: rows start on 16 bytes
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_addr(dst)),
+               "l"(map), "r"(0), "r"(row), "r"(page), "r"(smem_addr(bar))
+               : "memory");
+}
+
+// Host: the codes as [page][head * slot][component], boxes of `tokens` rows of DP bytes (components behind D read as zero codes).
+lantern_status code_map(CUtensorMap* map, const void* code, const lantern_cache* c, int DP, int tokens);
+
+}  // namespace lantern
