@@ -1,4 +1,5 @@
-"""Binding of liblantern.so: argument marshalling only, through ctypes and, for the usual form of verify(), natively (csrc/call.cpp).
+"""Binding of liblantern.so: argument marshalling only, through ctypes and, for the usual form of verify() and of the cache operators
+(cache.py), natively (csrc/call.cpp).
 
 Functions mirror the C entry points of include/lantern.h.  Tensors must live on a CUDA device;
 there is no CPU path: a missing library or a CPU tensor raises.
@@ -104,9 +105,12 @@ def load_library():
     lib.lantern_verify.restype = i32
     lib.lantern_verify.argtypes = [vp, vp, i32, f32, i32, f32, vp, vp, vp, i32, f32, vp, i32, i32, i32,
                                    vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    from . import cache
+    operators = cache.declare(lib)
     call = _load_call()
     if call is not None:
         call.bind(ctypes.cast(lib.lantern_verify_ex, ctypes.c_void_p).value)
+        call.bind_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in operators))
     _call = call
     _lib = lib      # (last: what another thread finds loaded is loaded whole)
     return lib

@@ -1,6 +1,7 @@
 """Binding of the cache operators of include/lantern.h: rotary positions, the paged 8-bit cache of keys and values, attention to it.
 
-Like binding.py it marshals arguments and does nothing else; there is no CPU path.
+Like binding.py it marshals arguments and does nothing else; there is no CPU path.  Calls in their usual form (outputs and workspace
+given, no stream argument, tensors on the current device) go to the library natively, all others through ctypes.
 """
 from __future__ import annotations
 
@@ -9,6 +10,7 @@ from typing import Optional, Sequence
 
 import torch
 
+from . import binding
 from .binding import BF16, F32, LanternError, _ptr, _stream_ptr, load_library
 
 MAX_AXES = 4
@@ -26,28 +28,28 @@ class _RotationStruct(ctypes.Structure):
 
 
 _Strides = ctypes.c_int64 * 3
-_declared = False
 
 
-def _lib():
-    global _declared
-    lib = load_library()
-    if not _declared:
-        vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
-        lib.lantern_rotary.restype = i32
-        lib.lantern_rotary.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp]
-        lib.lantern_cache_append.restype = i32
-        lib.lantern_cache_append.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
-        lib.lantern_cache_attention_workspace_bytes.restype = sz
-        lib.lantern_cache_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, vp, i32]
-        lib.lantern_cache_attention.restype = i32
-        lib.lantern_cache_attention.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, f32, vp, vp, sz, vp]
-        lib.lantern_cache_keep.restype = i32
-        lib.lantern_cache_keep.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp]
-        lib.lantern_cache_read.restype = i32
-        lib.lantern_cache_read.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp]
-        _declared = True
-    return lib
+def declare(lib):
+    """Argument types of the operators' entry points; returns them in the order that the native part of the binding takes them in."""
+    vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+    lib.lantern_rotary.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp]
+    lib.lantern_cache_append.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    lib.lantern_cache_attention_workspace_bytes.restype = sz
+    lib.lantern_cache_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, vp, i32]
+    lib.lantern_cache_attention.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, f32, vp, vp, sz, vp]
+    lib.lantern_cache_keep.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.lantern_cache_read.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    operators = (lib.lantern_rotary, lib.lantern_cache_append, lib.lantern_cache_attention, lib.lantern_cache_keep, lib.lantern_cache_read)
+    for f in operators:
+        f.restype = i32
+    return operators
+
+
+def _native(stream):
+    """The native part of the binding for a call on the current stream, or None."""
+    load_library()
+    return binding._call if stream is None else None
 
 
 def _dtype(t: torch.Tensor, name: str) -> int:
@@ -83,7 +85,7 @@ def _index(t: Optional[torch.Tensor], shape, device, name: str):
 class KVCache:
     """A paged cache of one layer's keys and values in 8 bits: codes k, v [pages, heads, page_tokens, head_dim] float8_e4m3fn, and a
     scale for each page and head, k_scale, v_scale [pages, heads] float32 (see lantern_cache in include/lantern.h)."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page_tokens", "head_dim", "device", "_struct", "_at")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page_tokens", "head_dim", "device", "_struct", "_at", "_device")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         if k.dim() != 4 or k.shape != v.shape:
@@ -101,6 +103,7 @@ class KVCache:
         self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.pages, self.heads,
                                     self.page_tokens, self.head_dim)
         self._at = ctypes.addressof(self._struct)
+        self._device = k.get_device()
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_tokens: int, head_dim: int, device="cuda") -> "KVCache":
@@ -112,7 +115,7 @@ class KVCache:
 class Rotation:
     """Rotary frequencies: inv_freq [P] float32, the number of pairs of each axis, and which components make a pair -- (2j, 2j+1) if
     interleaved, else (j, j+P) (see lantern_rotation in include/lantern.h)."""
-    __slots__ = ("inv_freq", "sections", "interleaved")
+    __slots__ = ("inv_freq", "sections", "interleaved", "_struct", "_at", "_device")
 
     def __init__(self, inv_freq: torch.Tensor, sections: Sequence[int], *, interleaved: bool):
         sections = tuple(int(s) for s in sections)
@@ -122,15 +125,19 @@ class Rotation:
             raise ValueError("inv_freq must hold one frequency for each pair of the sections")
         _ptr(inv_freq, torch.float32, "inv_freq")
         self.inv_freq, self.sections, self.interleaved = inv_freq, sections, bool(interleaved)
+        n = len(sections)
+        self._struct = _RotationStruct(inv_freq.data_ptr(), None, n, int(interleaved), (ctypes.c_int32 * MAX_AXES)(*sections, *(0,) * (MAX_AXES - n)))
+        self._at = ctypes.addressof(self._struct)
+        self._device = inv_freq.get_device()
 
     def _bind(self, positions: torch.Tensor, B: int, R: int, device) -> _RotationStruct:
         if positions is None:
             raise ValueError("a rotation needs positions")
         if self.inv_freq.device != device:
             raise ValueError(f"inv_freq must be on {device}")
-        at = _index(positions, (len(self.sections), B, R), device, "positions")
-        n = len(self.sections)
-        return _RotationStruct(self.inv_freq.data_ptr(), at, n, int(self.interleaved), (ctypes.c_int32 * MAX_AXES)(*self.sections, *(0,) * (MAX_AXES - n)))
+        out = _RotationStruct.from_buffer_copy(self._struct)
+        out.positions = _index(positions, (len(self.sections), B, R), device, "positions")
+        return out
 
 
 def _check(rc: int, where: str) -> None:
@@ -142,12 +149,17 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, rotation: Rotation, *, inve
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_rotary: rows x [B, R, H, D] turned by positions [axes, B, R].  inverse=True turns back, which is also the gradient with
     respect to x of a gradient with respect to the result.  out: a tensor like x, or x itself; allocated if not given."""
-    lib = _lib()
-    px, xs = _rows(x, "x")
-    dtype = _dtype(x, "x")
+    lib, call = load_library(), _native(stream)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+    if call is not None and rotation is not None:
+        rc = call.rotary(x, positions, rotation._at, rotation._device, inverse, out)
+        if rc is not None:
+            _check(rc, "lantern_rotary")
+            return out
+    px, xs = _rows(x, "x")
+    dtype = _dtype(x, "x")
+    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("out must be like x")
     po, os_ = _rows(out, "out")
     if px == po and x.stride() != out.stride():
@@ -173,7 +185,12 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, table: torch.
     """lantern_cache_append: rows k, v [B, R, heads, D] become tokens lengths[b], lengths[b] + 1, ... of their sequences; keys are turned by
     positions [axes, B, R] on the way if a rotation is given.  table [B, blocks], lengths [B], counts [B] (rows that there are; None = R)
     and status [B] (fault bits are OR-ed into it) are int32."""
-    lib = _lib()
+    lib, call = load_library(), _native(stream)
+    if call is not None:
+        rc = call.append(k, v, cache._at, cache._device, table, lengths, counts, positions, None if rotation is None else rotation._at,
+                         None if rotation is None else rotation._device, status)
+        if rc is not None:
+            return _check(rc, "lantern_cache_append")
     pk, ks = _rows(k, "k")
     pv, vs = _rows(v, "v")
     dtype = _dtype(k, "k")
@@ -197,7 +214,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, table: torch.
 
 def cache_attention_workspace_bytes(B: int, R: int, q_heads: int, cache: KVCache, blocks: int, *, dtype: torch.dtype = torch.bfloat16) -> int:
     """lantern_cache_attention_workspace_bytes: scratch bytes of one cache_attention() call with a table of `blocks` columns."""
-    return int(_lib().lantern_cache_attention_workspace_bytes(BF16 if dtype == torch.bfloat16 else F32, B, R, q_heads, cache._at, blocks))
+    return int(load_library().lantern_cache_attention_workspace_bytes(BF16 if dtype == torch.bfloat16 else F32, B, R, q_heads, cache._at, blocks))
 
 
 def cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, *, counts: Optional[torch.Tensor] = None,
@@ -207,7 +224,12 @@ def cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, length
     """lantern_cache_attention: queries [B, R, q_heads, D] of the rows that cache_append() has just put behind the sequences' `lengths`
     tokens, attending to the tokens from starts[b] (None: 0) on and to their own ancestors (tree_parents [B, R-1] as in verify(); None =
     a chain, i.e. causal).  scale: None = head_dim ** -0.5.  Rows that `counts` leaves out stay as they are in `out`."""
-    lib = _lib()
+    lib, call = load_library(), _native(stream)
+    if call is not None and out is not None and workspace is not None:
+        rc = call.attention(q, cache._at, cache._device, table, lengths, counts, starts, tree_parents, scale, out, workspace, status)
+        if rc is not None:
+            _check(rc, "lantern_cache_attention")
+            return out
     pq, qs = _rows(q, "q")
     dtype = _dtype(q, "q")
     B, R, HQ, D = q.shape
@@ -246,15 +268,20 @@ def cache_keep(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, accep
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_cache_keep: after verify(), moves the accepted path's tokens behind the root's and returns the sequences' new lengths (the
     root's and the path's tokens counted).  accept_len [B], accept_path [B, N] as verify() gives them."""
-    lib = _lib()
+    lib, call = load_library(), _native(stream)
+    if out_lengths is None:
+        out_lengths = torch.empty_like(lengths)
+    if call is not None:
+        rc = call.keep(cache._at, cache._device, table, lengths, accept_len, accept_path, out_lengths, status)
+        if rc is not None:
+            _check(rc, "lantern_cache_keep")
+            return out_lengths
     if accept_path.dim() != 2:
         raise ValueError("accept_path must be [B, N]")
     B, N = accept_path.shape
     dev = cache.device
     pt, width = _table(cache, table, B)
     pl = _index(lengths, (B,), dev, "lengths")
-    if out_lengths is None:
-        out_lengths = torch.empty_like(lengths)
     with torch.cuda.device(dev):
         _check(lib.lantern_cache_keep(cache._at, pt, width, pl, _index(accept_len, (B,), dev, "accept_len"),
                                       _index(accept_path, (B, N), dev, "accept_path"), B, N, _index(out_lengths, (B,), dev, "out_lengths"),
@@ -267,7 +294,12 @@ def cache_read(cache: KVCache, table: torch.Tensor, first: torch.Tensor, rows: i
                stream: Optional[torch.cuda.Stream] = None):
     """lantern_cache_read: the keys and values [B, rows, heads, D] of tokens first[b], first[b] + 1, ... in bf16 or fp32 (out: a pair of
     such tensors).  Rows that `counts` leaves out stay as they are in `out`."""
-    lib = _lib()
+    lib, call = load_library(), _native(stream)
+    if call is not None and out is not None:
+        rc = call.read(cache._at, cache._device, table, first, rows, counts, *out, status)
+        if rc is not None:
+            _check(rc, "lantern_cache_read")
+            return out
     B, rows = int(table.shape[0]), int(rows)
     dev = cache.device
     shape = (B, rows, cache.heads, cache.head_dim)

@@ -476,7 +476,7 @@ static lantern_status check_attention(int dtype, int B, int R, int q_heads, cons
   if (B < 0 || R < 0 || q_heads < 1 || q_heads % c->heads != 0 || (tree && R > kMaxTreeRows)) return LANTERN_E_SHAPE;
   if (static_cast<int64_t>(R) * (q_heads / c->heads) > INT32_MAX / 2 || static_cast<int64_t>(B) * R > INT32_MAX) return LANTERN_E_SHAPE;
   const Division d = divide(B, R, q_heads, c, width);
-  if (d.units * d.splits > INT32_MAX) return LANTERN_E_SHAPE;
+  if (d.units * (d.splits > 16 ? d.splits : 16) > INT32_MAX) return LANTERN_E_SHAPE;
   return LANTERN_OK;
 }
 
@@ -491,8 +491,8 @@ static cudaError_t launch_attention(const AttendParams& P, const CUtensorMap& k,
   lantern_attention_kernel<ROWS, DP, BF16><<<static_cast<unsigned>(d.units * d.splits), CT, smem, st>>>(P, k, v);
   if ((e = cudaGetLastError()) != cudaSuccess || d.splits == 1) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(d.units));
-  cfg.blockDim = dim3(128);
+  cfg.gridDim = dim3(static_cast<unsigned>(d.units * (ROWS * 32 / kJoinThreads)));
+  cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -93,36 +93,58 @@ __device__ __forceinline__ void ancestor_bits(const AttendParams& P, const Unit&
   }
 }
 
-// Joins the parts of a unit: a CTA per unit, a thread per four components.
+// Joins the parts of a unit: a warp per row, a lane per four components; the weights of up to 32 parts are formed at once, a lane each.
+constexpr int kJoinThreads = 128;
 template <int ROWS, int DP, bool BF16>
-__global__ void __launch_bounds__(128) lantern_join_kernel(AttendParams P) {
+__global__ void __launch_bounds__(kJoinThreads) lantern_join_kernel(AttendParams P) {
   using T = typename Row<BF16>::T;
+  constexpr int kPerCta = kJoinThreads / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = blockIdx.x / (ROWS / kPerCta);
+  const int row = static_cast<int>(blockIdx.x % (ROWS / kPerCta)) * kPerCta + (threadIdx.x >> 5);
+  const Unit u = unit_of<ROWS>(P, unit, 0);
   grid_dependency_wait();
-  const Unit u = unit_of<ROWS>(P, blockIdx.x, 0);
-  if (!u.rows || u.parts == 1) return;
-  const int rows = min(ROWS, u.n * P.G - u.m0), per_row = P.D >> 2;
-  const int64_t base = static_cast<int64_t>(blockIdx.x) * P.splits;
-  for (int i = threadIdx.x; i < rows * per_row; i += 128) {
-    const int row = i / per_row, d = (i - row * per_row) * 4;
-    float M = -INFINITY;
-    for (int s = 0; s < u.parts; ++s) M = fmaxf(M, P.part_ml[(base + s) * ROWS + row].x);
-    const float sub = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s = 0; s < u.parts; ++s) {
-      const float2 ml = P.part_ml[(base + s) * ROWS + row];
-      const float w = ex2_approx(ml.x - sub);
-      const float4 o = *reinterpret_cast<const float4*>(P.parts + ((base + s) * ROWS + row) * DP + d);
-      L += ml.y * w;
-      acc.x += o.x * w, acc.y += o.y * w, acc.z += o.z * w, acc.w += o.w * w;
-    }
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;   // (nothing seen: zeros; NaN stays)
-    const int m = u.m0 + row, r = m / P.G;
-    T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (m - r * P.G)) * P.D + d;
-    const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-    if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(bf16x2_round(v[0], v[1]), bf16x2_round(v[2], v[3]));
-    else *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+  if (!u.rows || u.parts == 1 || row >= u.n * P.G - u.m0) return;
+  const int64_t base = unit * P.splits;
+  float M = -INFINITY;
+  bool odd = false;
+  for (int s = lane; s < u.parts; s += 32) {
+    const float2 ml = P.part_ml[(base + s) * ROWS + row];
+    M = fmaxf(M, ml.x);
+    odd |= ml.y != ml.y;
   }
+  M = warp_max(M);
+  odd = __any_sync(kFull, odd);
+  const float sub = M == -INFINITY ? 0.0f : M;
+  float L = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const int d = lane * 4;
+  for (int s0 = 0; s0 < u.parts; s0 += 32) {
+    float w = 0.0f;
+    if (s0 + lane < u.parts) {
+      const float2 ml = P.part_ml[(base + s0 + lane) * ROWS + row];
+      w = ex2_approx(ml.x - sub);
+      L += ml.y * w;
+    }
+    const int n = min(32, u.parts - s0);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float wi = __shfl_sync(kFull, w, i);
+      if (d < P.D) {
+        const float4 o = *reinterpret_cast<const float4*>(P.parts + ((base + s0 + i) * ROWS + row) * DP + d);
+        acc.x += o.x * wi, acc.y += o.y * wi, acc.z += o.z * wi, acc.w += o.w * wi;
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(kFull, L, o);
+  const float inv = odd ? __int_as_float(0x7fffffff) : (L == 0.0f ? 0.0f : 1.0f / L);   // (nothing seen: zeros)
+  if (d >= P.D) return;
+  const int m = u.m0 + row, r = m / P.G;
+  T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (m - r * P.G)) * P.D + d;
+  const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+  if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(bf16x2_round(v[0], v[1]), bf16x2_round(v[2], v[3]));
+  else *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
 __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int row, int page, uint64_t* bar) {   // x = 0: rows start on 16 bytes

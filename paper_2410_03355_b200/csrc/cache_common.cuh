@@ -109,17 +109,18 @@ struct Rotation {
   int pairs, interleaved;
   int ends[LANTERN_MAX_AXES];   // running sums of the sections; axes that are not used end at `pairs`
 };
-// cos and sin of position * inv_freq: the product and its remainder modulo a full turn in double precision, so that the angle that
-// reaches single precision lies within half a turn and is off by at most 2^-25 of one, however far the position.
+// cos and sin of position * inv_freq: the product and its remainder modulo a full turn in double precision, so that the angle lies within half
+// a turn, however far the position; what rounding it to single precision leaves (at most 2^-25 half turns) turns the result once more.
 __device__ __forceinline__ float2 turn(const Rotation& R, int64_t token, int j) {
   const int axis = (j >= R.ends[0]) + (j >= R.ends[1]) + (j >= R.ends[2]);
   const double turns = static_cast<double>(__ldg(R.positions + axis * R.plane + token)) * static_cast<double>(__ldg(R.inv_freq + j)) *
                        0.15915494309189533577;   // 1 / (2 pi)
+  const double halves = 2.0 * (turns - rint(turns));
+  const float near = static_cast<float>(halves), rest = static_cast<float>(halves - near) * 3.14159265f;
   float s, c;
-  sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &s, &c);
-  return make_float2(c, s);
+  sincospif(near, &s, &c);
+  return make_float2(__fmaf_rn(-s, rest, c), __fmaf_rn(c, rest, s));
 }
-
 // The two components of a turned pair, each with one fused rounding and one of the product, so that every kernel and path gives the same bits.
 __device__ __forceinline__ float turned_low(float a, float b, float2 cs) { return __fmaf_rn(a, cs.x, -__fmul_rn(b, cs.y)); }
 __device__ __forceinline__ float turned_high(float a, float b, float2 cs) { return __fmaf_rn(b, cs.x, __fmul_rn(a, cs.y)); }

@@ -29,28 +29,28 @@ def ref(s):
 
 def append(c=None, k=AT, v=AT, dtype=lt.BF16, B=2, R=3, ks=None, vs=None, table=AT, width=4, lengths=AT, rot=None):
     c, ks, vs = c or cache(), ks or strides(), vs or strides()
-    return binding._lib().lantern_cache_append(k, v, dtype, B, R, ks, vs, ref(c), table, width, lengths, None, ref(rot), None, None)
+    return lt.load_library().lantern_cache_append(k, v, dtype, B, R, ks, vs, ref(c), table, width, lengths, None, ref(rot), None, None)
 
 
 def attention(c=None, q=AT, out=AT, dtype=lt.BF16, B=2, R=3, HQ=8, table=AT, width=4, lengths=AT, parents=None, scale=0.1, ws=None, ws_bytes=0):
     c = c or cache()
-    return binding._lib().lantern_cache_attention(q, out, dtype, B, R, HQ, strides(), ref(c), table, width, lengths, None, None, parents, scale, None,
+    return lt.load_library().lantern_cache_attention(q, out, dtype, B, R, HQ, strides(), ref(c), table, width, lengths, None, None, parents, scale, None,
                                                   ws, ws_bytes, None)
 
 
 def keep(c=None, table=AT, width=4, lengths=AT, accept=AT, path=AT, B=2, N=3, out=AT):
     c = c or cache()
-    return binding._lib().lantern_cache_keep(ref(c), table, width, lengths, accept, path, B, N, out, None, None)
+    return lt.load_library().lantern_cache_keep(ref(c), table, width, lengths, accept, path, B, N, out, None, None)
 
 
 def read(c=None, table=AT, width=4, first=AT, B=2, R=3, dtype=lt.BF16, k=AT, v=AT):
     c = c or cache()
-    return binding._lib().lantern_cache_read(ref(c), table, width, first, None, B, R, dtype, k, v, None, None)
+    return lt.load_library().lantern_cache_read(ref(c), table, width, first, None, B, R, dtype, k, v, None, None)
 
 
 def rotary(x=AT, out=AT, dtype=lt.BF16, B=2, R=3, H=4, D=64, rot=None):
     rot = rot or rotation()
-    return binding._lib().lantern_rotary(x, out, dtype, B, R, H, D, strides(), strides(), ref(rot), 0, None)
+    return lt.load_library().lantern_rotary(x, out, dtype, B, R, H, D, strides(), strides(), ref(rot), 0, None)
 
 
 @pytest.mark.parametrize("call", [append, attention, keep, read])
