@@ -30,19 +30,10 @@ __device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t roun
 }
 __device__ __forceinline__ uint32_t without_nan(uint32_t codes) { return codes & ~__vcmpeq4(codes & 0x7f7f7f7fu, 0x7f7f7f7fu); }
 
-// byte offset of a 16-byte chunk of a token's codes within a stage's keys or values, as the swizzled copy leaves it
-template <int DP>
-__device__ __forceinline__ int chunk_at(int token, int chunk) {
-  return DP == 128 ? token * 128 + ((chunk ^ (token & 7)) << 4) : token * 64 + ((chunk ^ ((token >> 1) & 3)) << 4);
-}
+constexpr int kTile = 64;
 
-template <int DP>
-struct AttendShared {
-  uint64_t full[kStages], empty[kStages];
-  float scale[kStages][2][kTileTokens / 16];
+struct AttendShared : StageShared<kTile, kStages> {
   float ml[4][16][2];
-  float vref[4];
-  int fault;
 };
 
 // ROWS = 16: the four warps take 16 tokens of a stage each, for the same 16 rows.  ROWS = 64: each takes 16 rows and all tokens.
@@ -53,14 +44,14 @@ __global__ void __launch_bounds__(CT) lantern_attention_kernel(AttendParams P, c
   constexpr int TERMS = BF16 ? 1 : 2;         // halves that a query or probability goes in as
   constexpr int KS = DP / 16, NT = DP / 8;    // steps of the scores' products, column tiles of the output
   constexpr int EL = DP / 4;                  // components of a row that a lane holds, side by side
-  constexpr int kStageBytes = 2 * kTileTokens * DP;
+  constexpr int kStageBytes = 2 * kTile * DP;
   constexpr bool WIDE = ROWS == 64;
   extern __shared__ __align__(1024) uint8_t smem[];
-  AttendShared<DP>& S = *reinterpret_cast<AttendShared<DP>*>(smem + kStages * kStageBytes);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(smem + kStages * kStageBytes + sizeof(AttendShared<DP>));
+  AttendShared& S = *reinterpret_cast<AttendShared*>(smem + kStages * kStageBytes);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(smem + kStages * kStageBytes + sizeof(AttendShared));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t unit = blockIdx.x / P.splits;
-  const Unit u = unit_of<ROWS>(P, unit, static_cast<int>(blockIdx.x - unit * P.splits));
+  const Unit u = unit_of(P, ROWS, kTile, unit, static_cast<int>(blockIdx.x - unit * P.splits));
   grid_dependents_launch();
   if (!u.rows || u.split >= u.parts) return;
   const int words = (P.R + 31) >> 5, first_row = u.m0 / P.G;
@@ -81,49 +72,7 @@ __global__ void __launch_bounds__(CT) lantern_attention_kernel(AttendParams P, c
   __syncthreads();                          // (the producer may add to it from here on)
 
   if (warp == 4) {   // ---- producer ----
-    const int sub = min(P.S, kTileTokens), subs = kTileTokens / sub;
-    int it = 0;
-    for (int tile = u.lo; tile < stop; ++tile, ++it) {
-      const int stage = it % kStages, round = it / kStages;
-      const int token = (u.tile0 + tile) * kTileTokens + lane * sub;
-      const bool mine = lane < subs && token < u.end && token + sub > u.begin;
-      int page = 0;
-      if (mine) {
-        page = __ldg(P.table + static_cast<int64_t>(u.b) * P.width + token / P.S);
-        if (page < 0 || page >= P.pages) {
-          atomicOr(&S.fault, LANTERN_ST_BAD_BLOCK);
-          page = 0;
-        }
-      }
-      float ks = 1.0f, vs = 1.0f;
-      if (mine) {
-        const int64_t block = static_cast<int64_t>(page) * P.heads + u.h;
-        ks = __ldg(P.k_scale + block), vs = __ldg(P.v_scale + block);
-      }
-      int ok = 1;
-      if (round > 0) ok = mbar_wait(&S.empty[stage], (round - 1) & 1);
-      if (!__all_sync(kFull, ok)) {
-        if (lane == 0) atomicOr(&S.fault, LANTERN_ST_INTERNAL);
-        break;
-      }
-      if (lane < subs)
-        for (int i = 0; i < sub / 16; ++i) {
-          S.scale[stage][0][lane * (sub / 16) + i] = ks;
-          S.scale[stage][1][lane * (sub / 16) + i] = vs;
-        }
-      __syncwarp();
-      const int copies = __popc(__ballot_sync(kFull, mine));
-      if (lane == 0) mbar_expect_tx(&S.full[stage], copies * 2 * sub * DP);
-      __syncwarp();
-      if (mine) {
-        uint8_t* at = smem + stage * kStageBytes + lane * sub * DP;
-        const int row = u.h * P.S + token % P.S;
-        tma_load(at, &kmap, row, page, &S.full[stage]);
-        tma_load(at + kTileTokens * DP, &vmap, row, page, &S.full[stage]);
-      }
-    }
-    // nothing may be in flight when the CTA ends: the last copies into every stage
-    for (int i = max(0, it - kStages); i < it; ++i) mbar_wait(&S.full[i % kStages], (i / kStages) & 1);
+    produce<kTile, DP, kStages>(P, u, stop, smem, S, &kmap, &vmap, lane);
     __syncthreads();
     return;
   }
@@ -321,16 +270,16 @@ __global__ void __launch_bounds__(CT) lantern_attention_kernel(AttendParams P, c
   int it = 0;
   for (int tile = u.lo; tile < stop; ++tile, ++it) {
     const int stage = it % kStages;
-    if (!__all_sync(kFull, mbar_wait(&S.full[stage], (it / kStages) & 1))) {
+    if (!__all_sync(kFull, await(&S.full[stage], (it / kStages) & 1))) {
       if (lane == 0) atomicOr(&S.fault, LANTERN_ST_INTERNAL);
       break;
     }
     const uint8_t* keys = smem + stage * kStageBytes;
 #pragma unroll 1
     for (int sb = WIDE ? 0 : warp; sb < (WIDE ? 4 : warp + 1); ++sb) {
-      const int token0 = (u.tile0 + tile) * kTileTokens + sb * 16;
+      const int token0 = (u.tile0 + tile) * kTile + sb * 16;
       if (token0 >= u.end || token0 + 16 <= u.begin || token0 > u.len + warp_last) continue;
-      step(keys, keys + kTileTokens * DP, token0, sb, S.scale[stage][0][sb], S.scale[stage][1][sb]);
+      step(keys, keys + kTile * DP, token0, sb, S.scale[stage][0][sb], S.scale[stage][1][sb]);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&S.empty[stage]);
@@ -448,20 +397,15 @@ lantern_status code_map(CUtensorMap* map, const void* code, const lantern_cache*
              : LANTERN_E_CUDA;
 }
 
-// How a call's rows and tokens are divided.
-struct Division {
-  int rows, DP;          // rows per unit; padded components
-  int row_tiles, splits, least;
-  int64_t units;
-};
 static Division divide(int B, int R, int q_heads, const lantern_cache* c, int width) {
   Division d;
   const int64_t G = q_heads / c->heads, M = G * R;
-  d.rows = M <= 16 ? 16 : 64;
   d.DP = c->head_dim <= 64 ? 64 : 128;
+  d.rows = M <= 16 ? 16 : M <= 64 ? 64 : 128;
+  d.tile = d.rows > 16 && d.DP == 128 ? 128 : kTile;
   d.row_tiles = static_cast<int>((M + d.rows - 1) / d.rows);
   d.units = static_cast<int64_t>(B) * c->heads * d.row_tiles;
-  const int64_t slots = 148 * 2, tiles = (static_cast<int64_t>(width) * c->page_tokens + kTileTokens - 1) / kTileTokens;
+  const int64_t slots = 148 * 2, tiles = (static_cast<int64_t>(width) * c->page_tokens + d.tile - 1) / d.tile;
   d.least = 2;
   int64_t splits = d.units >= slots ? 1 : (2 * slots + d.units - 1) / (d.units > 0 ? d.units : 1);
   if (splits > tiles / d.least) splits = tiles / d.least;
@@ -482,7 +426,7 @@ static lantern_status check_attention(int dtype, int B, int R, int q_heads, cons
 
 template <int ROWS, int DP, bool BF16>
 static cudaError_t launch_attention(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, cudaStream_t st) {
-  constexpr size_t kFixed = kStages * 2 * kTileTokens * DP + sizeof(AttendShared<DP>);
+  constexpr size_t kFixed = kStages * 2 * kTile * DP + sizeof(AttendShared);
   const size_t words = (P.R + 31) / 32, rows = (ROWS + P.G - 1) / P.G + 1;
   const size_t smem = kFixed + (P.parents ? (rows * words + P.R) * 4 : 0);
   static DeviceFlags ready;
@@ -490,16 +434,7 @@ static cudaError_t launch_attention(const AttendParams& P, const CUtensorMap& k,
   if (e != cudaSuccess) return e;
   lantern_attention_kernel<ROWS, DP, BF16><<<static_cast<unsigned>(d.units * d.splits), CT, smem, st>>>(P, k, v);
   if ((e = cudaGetLastError()) != cudaSuccess || d.splits == 1) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(d.units * (ROWS * 32 / kJoinThreads)));
-  cfg.blockDim = dim3(kJoinThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, lantern_join_kernel<ROWS, DP, BF16>, P);
+  return launch_join<DP, BF16>(P, d, st);
 }
 
 }  // namespace lantern
@@ -558,16 +493,12 @@ extern "C" lantern_status lantern_cache_attention(const void* q, void* out, int 
   P.vec = aligned16(q, qs, size);
   P.scale_log2 = scale * 1.44269504088896340736f;
   CUtensorMap km, vm;
-  const int tokens = P.S < kTileTokens ? P.S : kTileTokens;
+  const int tokens = P.S < d.tile ? P.S : d.tile;
   if ((bad = code_map(&km, cache->k_code, cache, d.DP, tokens)) != LANTERN_OK || (bad = code_map(&vm, cache->v_code, cache, d.DP, tokens)) != LANTERN_OK) return bad;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (d.rows == 16) {
-    if (d.DP == 64) e = bf ? launch_attention<16, 64, true>(P, km, vm, d, st) : launch_attention<16, 64, false>(P, km, vm, d, st);
-    else e = bf ? launch_attention<16, 128, true>(P, km, vm, d, st) : launch_attention<16, 128, false>(P, km, vm, d, st);
-  } else {
-    if (d.DP == 64) e = bf ? launch_attention<64, 64, true>(P, km, vm, d, st) : launch_attention<64, 64, false>(P, km, vm, d, st);
-    else e = bf ? launch_attention<64, 128, true>(P, km, vm, d, st) : launch_attention<64, 128, false>(P, km, vm, d, st);
-  }
+  if (d.rows > 16) e = launch_attention_wide(P, km, vm, d, bf, st);
+  else if (d.DP == 64) e = bf ? launch_attention<16, 64, true>(P, km, vm, d, st) : launch_attention<16, 64, false>(P, km, vm, d, st);
+  else e = bf ? launch_attention<16, 128, true>(P, km, vm, d, st) : launch_attention<16, 128, false>(P, km, vm, d, st);
   return e == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
 }

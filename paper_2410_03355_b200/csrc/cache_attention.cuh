@@ -7,8 +7,6 @@
 
 namespace lantern {
 
-constexpr int kTileTokens = 64;   // tokens per step of the long axis
-
 struct AttendParams {
   const void* q;
   void* out;
@@ -41,8 +39,8 @@ struct Unit {
   int fault;
   bool rows;             // there are rows to answer
 };
-template <int ROWS>
-__device__ __forceinline__ Unit unit_of(const AttendParams& P, int64_t unit, int split) {
+// (rows of a unit, tokens of a stage)
+__device__ __forceinline__ Unit unit_of(const AttendParams& P, int ROWS, int TILE, int64_t unit, int split) {
   Unit u;
   u.split = split;
   const int mt = static_cast<int>(unit % P.row_tiles);
@@ -62,8 +60,8 @@ __device__ __forceinline__ Unit unit_of(const AttendParams& P, int64_t unit, int
   const int first = u.m0 / P.G, last = min(u.n - 1, (u.m0 + ROWS - 1) / P.G);
   u.rows = first < u.n;
   u.end = u.fault ? u.begin : u.len + last + 1;   // (an ancestor has a smaller row: trees and chains alike)
-  u.tile0 = u.begin / kTileTokens;
-  const int tiles = u.end > u.begin ? (u.end + kTileTokens - 1) / kTileTokens - u.tile0 : 0;
+  u.tile0 = u.begin / TILE;
+  const int tiles = u.end > u.begin ? (u.end + TILE - 1) / TILE - u.tile0 : 0;
   const int per = max((tiles + P.splits - 1) / P.splits, P.least);
   u.parts = max(1, (tiles + per - 1) / per);
   u.lo = split * per;
@@ -95,14 +93,14 @@ __device__ __forceinline__ void ancestor_bits(const AttendParams& P, const Unit&
 
 // Joins the parts of a unit: a warp per row, a lane per four components; the weights of up to 32 parts are formed at once, a lane each.
 constexpr int kJoinThreads = 128;
-template <int ROWS, int DP, bool BF16>
-__global__ void __launch_bounds__(kJoinThreads) lantern_join_kernel(AttendParams P) {
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(kJoinThreads) lantern_join_kernel(AttendParams P, int ROWS, int TILE) {
   using T = typename Row<BF16>::T;
   constexpr int kPerCta = kJoinThreads / 32;
   const int lane = threadIdx.x & 31;
   const int64_t unit = blockIdx.x / (ROWS / kPerCta);
   const int row = static_cast<int>(blockIdx.x % (ROWS / kPerCta)) * kPerCta + (threadIdx.x >> 5);
-  const Unit u = unit_of<ROWS>(P, unit, 0);
+  const Unit u = unit_of(P, ROWS, TILE, unit, 0);
   grid_dependency_wait();
   if (!u.rows || u.parts == 1 || row >= u.n * P.G - u.m0) return;
   const int64_t base = unit * P.splits;
@@ -152,6 +150,123 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int 
                "l"(map), "r"(0), "r"(row), "r"(page), "r"(smem_addr(bar))
                : "memory");
 }
+
+// Bounded wait for a phase without a suspension hint: with one, a thread that has to wait sleeps, and a tile's few waits in a row cost more
+// than its products.
+__device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity) {
+  const uint32_t a = smem_addr(bar);
+  for (uint32_t i = 0; i < (1u << 22); ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(a), "r"(parity)
+        : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+
+// What the producer and the warps that multiply share.
+template <int TILE, int STAGES>
+struct StageShared {
+  uint64_t full[STAGES], empty[STAGES];
+  float scale[STAGES][2][TILE / 16];   // of every 16 tokens: keys, values
+  int fault;
+};
+// byte offset of a 16-byte chunk of a token's codes within a stage's keys or values, as the swizzled copy leaves it
+template <int DP>
+__device__ __forceinline__ int chunk_at(int token, int chunk) {
+  return DP == 128 ? token * 128 + ((chunk ^ (token & 7)) << 4) : token * 64 + ((chunk ^ ((token >> 1) & 3)) << 4);
+}
+// One lane's box of a stage: where its tokens are, and their scales.
+struct Box {
+  int page, mine;   // mine: some row sees one of its tokens
+  float ks, vs;
+};
+template <int TILE>
+__device__ __forceinline__ Box look_up(const AttendParams& P, const Unit& u, int tile, int sub, int stop, int* fault) {
+  Box x{0, 0, 1.0f, 0.0f};
+  const int64_t token = static_cast<int64_t>(u.tile0 + tile) * TILE + sub;
+  x.mine = tile < stop && token < u.end && token + min(P.S, TILE) > u.begin;
+  if (x.mine) {
+    x.page = __ldg(P.table + static_cast<int64_t>(u.b) * P.width + token / P.S);
+    if (x.page < 0 || x.page >= P.pages) {
+      atomicOr(fault, LANTERN_ST_BAD_BLOCK);
+      x.page = 0;
+    }
+    const int64_t block = static_cast<int64_t>(x.page) * P.heads + u.h;
+    x.ks = __ldg(P.k_scale + block), x.vs = __ldg(P.v_scale + block);
+  }
+  return x;
+}
+// The producer warp: tiles [u.lo, stop) of the unit's tokens, keys and values, into the stages, block by block through the table.  A lane per
+// box; the table and the scales are looked up for as many stages as there are lanes, one batch ahead, because a stage's two
+// dependent reads take longer than its copy.
+template <int TILE, int DP, int STAGES>
+__device__ __forceinline__ void produce(const AttendParams& P, const Unit& u, int stop, uint8_t* stages, StageShared<TILE, STAGES>& S, const CUtensorMap* kmap,
+                                        const CUtensorMap* vmap, int lane) {
+  const int sub = min(P.S, TILE), subs = TILE / sub, batch = 32 / subs;   // tokens of a box, boxes of a stage, stages of a batch
+  const int my_stage = lane / subs, my_sub = (lane - my_stage * subs) * sub;
+  Box next = look_up<TILE>(P, u, u.lo + my_stage, my_sub, stop, &S.fault);
+  int it = 0;
+  for (int tile = u.lo; tile < stop; ++tile, ++it) {
+    const int in_batch = it % batch;
+    Box x;
+    if (in_batch == 0) {
+      x = next;
+      next = look_up<TILE>(P, u, tile + batch + my_stage, my_sub, stop, &S.fault);
+    }
+    const int stage = it % STAGES, round = it / STAGES;
+    if (!__all_sync(kFull, round == 0 || await(&S.empty[stage], (round - 1) & 1))) {
+      if (lane == 0) atomicOr(&S.fault, LANTERN_ST_INTERNAL);
+      break;
+    }
+    const bool turn = my_stage == in_batch, mine = turn && x.mine;
+    if (turn)
+      for (int i = 0; i < sub / 16; ++i) {
+        S.scale[stage][0][my_sub / 16 + i] = x.ks;
+        S.scale[stage][1][my_sub / 16 + i] = x.vs;
+      }
+    const int copies = __popc(__ballot_sync(kFull, mine));   // (at least one: every tile has a token that some row sees)
+    if (lane == 0) mbar_expect_tx(&S.full[stage], copies * 2 * sub * DP);
+    __syncwarp();
+    if (mine) {
+      uint8_t* at = stages + (stage * 2 * TILE + my_sub) * DP;
+      const int row = u.h * P.S + ((u.tile0 + tile) * TILE + my_sub) % P.S;
+      tma_load(at, kmap, row, x.page, &S.full[stage]);
+      tma_load(at + TILE * DP, vmap, row, x.page, &S.full[stage]);
+    }
+  }
+  // nothing may be in flight when the CTA ends: the last copies into every stage
+  for (int i = max(0, it - STAGES); i < it; ++i) await(&S.full[i % STAGES], (i / STAGES) & 1);
+}
+
+// Host: how a call's rows and tokens are divided.
+struct Division {
+  int rows, tile, DP;    // rows per unit; tokens per stage; padded components
+  int row_tiles, splits, least;
+  int64_t units;
+};
+
+template <int DP, bool BF16>
+static cudaError_t launch_join(const AttendParams& P, const Division& d, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(d.units * (d.rows * 32 / kJoinThreads)));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, lantern_join_kernel<DP, BF16>, P, d.rows, d.tile);
+}
+
+// More than 16 rows of a sequence and cache head (cache_attention_wide.cu).
+cudaError_t launch_attention_wide(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, bool bf16, cudaStream_t st);
 
 // Host: the codes as [page][head * slot][component], boxes of `tokens` rows of DP bytes (components behind D read as zero codes).
 lantern_status code_map(CUtensorMap* map, const void* code, const lantern_cache* c, int DP, int tokens);
