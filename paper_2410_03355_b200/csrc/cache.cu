@@ -69,6 +69,49 @@ __device__ __forceinline__ Span append_span(const AppendParams& P, int b, int j)
   return s;
 }
 
+// Eight components as they lie in memory.
+template <bool BF16>
+struct Raw {
+  uint4 w[BF16 ? 1 : 2];
+};
+template <bool BF16>
+__device__ __forceinline__ Raw<BF16> raw8(const typename Row<BF16>::T* p) {
+  Raw<BF16> r;
+#pragma unroll
+  for (int i = 0; i < (BF16 ? 1 : 2); ++i) r.w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ void widen8(const Raw<BF16>& r, float (&v)[8]) {
+  if constexpr (BF16) {
+    bf16x2_widen(r.w[0].x, v[0], v[1]), bf16x2_widen(r.w[0].y, v[2], v[3]), bf16x2_widen(r.w[0].z, v[4], v[5]), bf16x2_widen(r.w[0].w, v[6], v[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      v[4 * i] = __uint_as_float(r.w[i].x), v[4 * i + 1] = __uint_as_float(r.w[i].y), v[4 * i + 2] = __uint_as_float(r.w[i].z), v[4 * i + 3] = __uint_as_float(r.w[i].w);
+  }
+}
+// Eight keys turned: v their components from d on, o their partners' in the other half (if not interleaved).
+__device__ __forceinline__ void turn8(const Rotation& rot, int d, const float2* table, float (&v)[8], const float (&o)[8]) {
+  const int pairs = rot.pairs;
+  if (rot.interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      if (d + i < 2 * pairs) {
+        const float2 w = table[(d + i) >> 1];
+        const float a = v[i], b = v[i + 1];
+        v[i] = turned_low(a, b, w);
+        v[i + 1] = turned_high(a, b, w);
+      }
+    }
+  } else if (d < 2 * pairs) {
+    const bool lower = d < pairs;
+    const float2* w = table + (lower ? d : d - pairs);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = lower ? turned_low(v[i], o[i], w[i]) : turned_high(o[i], v[i], w[i]);
+  }
+}
+
 // Components [d, d + 8) of a row of keys (turned) or values.  table: cosines and sines of the row's pairs, NULL = not rotated.
 template <bool BF16>
 __device__ __forceinline__ void new_values(const AppendParams& P, const typename Row<BF16>::T* p, int d, const float2* table, float (&v)[8]) {
@@ -114,19 +157,31 @@ __device__ __forceinline__ void new_values(const AppendParams& P, const typename
     }
   }
 }
-// largest finite magnitude; `odd` is set if one of them is not finite, which then becomes NaN
+// Largest finite magnitude; `odd` is set if one of them is not finite, which then becomes NaN.  (As integers, magnitudes order like floats and
+// everything that is not finite comes last.)
 __device__ __forceinline__ float magnitude(float (&v)[8], int& odd) {
-  float m = 0.0f;
+  uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (fabsf(v[i]) < __int_as_float(0x7f800000)) {
-      m = fmaxf(m, fabsf(v[i]));
-    } else {
-      odd = 1;
-      v[i] = __int_as_float(0x7fffffff);
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  if (m >= 0x7f800000u) {
+    odd = 1;
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t x = __float_as_uint(v[i]) & 0x7fffffffu;
+      if (x < 0x7f800000u) m = max(m, x);
+      else v[i] = __int_as_float(0x7fffffff);
     }
   }
-  return m;
+  return __uint_as_float(m);
+}
+// eight values' codes under a scale
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], const Divider& over) {
+  if (over.exact) {
+    const float k = over.inverse;
+    return make_uint2(encode4(v[0] * k, v[1] * k, v[2] * k, v[3] * k), encode4(v[4] * k, v[5] * k, v[6] * k, v[7] * k));
+  }
+  return make_uint2(encode4(over(v[0]), over(v[1]), over(v[2]), over(v[3])), encode4(over(v[4]), over(v[5]), over(v[6]), over(v[7])));
 }
 // the scale that the block gets
 __device__ __forceinline__ float new_scale(float amax, float old, bool held, int& odd) {
@@ -139,38 +194,76 @@ __device__ __forceinline__ float new_scale(float amax, float old, bool held, int
   return fmaxf(need, old);
 }
 
-// A CTA per touched block and run of heads: the block's angles are formed once, then every head's keys and values go through registers, U units of
-// eight components per thread: maximum over the block, scale, codes.  Bound by HBM.
+// A CTA per touched block, run of heads and kind (keys or values): a block's angles are formed once for the heads of the run, then every head goes through
+// registers, U units of eight components per thread: maximum over the block, scale, codes.  Bound by the latency of a head's reads, the
+// maximum and the writes one after the other, and (keys) by the angles' arithmetic.
 constexpr int AT = 256;
 template <bool BF16, int U>
-__global__ void __launch_bounds__(AT) lantern_append_kernel(AppendParams P) {
+__global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) lantern_append_kernel(AppendParams P) {
   using T = typename Row<BF16>::T;
   extern __shared__ float2 angles[];   // [new slots][pairs]
   __shared__ float most[2][AT / 32];
+  __shared__ uint64_t steps[kMaxHeadDim / 2];
   const int b = blockIdx.z, j = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int h0 = blockIdx.x * P.heads_per_cta, h1 = min(h0 + P.heads_per_cta, P.c.heads);
+  const int which = blockIdx.x & 1, h0 = (blockIdx.x >> 1) * P.heads_per_cta, h1 = min(h0 + P.heads_per_cta, P.c.heads);
   const Span s = append_span(P, b, j);
   if (s.fault && tid == 0 && P.status) atomicOr(P.status + b, s.fault);
   const int n = s.high - s.low;
   if (s.fault || n <= 0) return;
-  const bool rotate = P.rot.inv_freq != nullptr;
-  const int pairs = rotate ? P.rot.pairs : 1;
-  if (rotate)
-    for (int i = tid; i < n * pairs; i += AT) angles[i] = turn(P.rot, static_cast<int64_t>(b) * P.R + s.row + i / pairs, i % pairs);
-  const int D = P.c.D, per_row = D >> 3, units = n * per_row;
+  const bool turns = P.rot.inv_freq != nullptr && which == 0;
+  const int pairs = turns ? P.rot.pairs : 1;
+  if (turns) {
+    for (int i = tid; i < pairs; i += AT) steps[i] = turn_step(P.rot, i);
+    __syncthreads();
+    const int at_once = AT / pairs, t0 = tid / pairs, k = tid - t0 * pairs;   // (at most 64 pairs)
+    const uint64_t step = steps[k];
+    if (t0 < at_once)
+#pragma unroll 2
+      for (int t = t0; t < n; t += at_once) angles[t * pairs + k] = turn_by(step, position_of(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, k));
+  }
+  // A thread keeps its eight components d.. of a row and goes through rows t0, t0 + at_once, ...
+  const int D = P.c.D, per_row = D >> 3, at_once = AT / per_row, t0 = tid / per_row, d = (tid - t0 * per_row) * 8;
+  const bool works = t0 < at_once;
+  const bool partners = turns && !P.rot.interleaved;
+  const int partner = d < pairs ? pairs : d < 2 * pairs ? -pairs : 0;   // where the other half of the pairs is
   int odd = 0, turn_of = 0;
   for (int h = h0; h < h1; ++h) {
-    for (int which = 0; which < 2; ++which) {
+    {
       const T* x = static_cast<const T*>(P.x[which]) + b * P.xs[which].b + h * P.xs[which].h;
       float v[U][8], m = 0.0f;
-      if (turn_of == 0) __syncthreads();   // the angles are there
+      if (P.vec && (!partners || pairs % 8 == 0)) {   // all reads of the head are under way before the first is used
+        Raw<BF16> own[U], other[U];
+        const T* p = x + s.row * P.xs[which].r + d;
+        const int64_t stride = P.xs[which].r;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = tid + u * AT;
-        if (i < units) {
-          const int t = i / per_row;
-          new_values<BF16>(P, x + (s.row + t) * P.xs[which].r, (i - t * per_row) * 8, rotate && which == 0 ? angles + t * pairs : nullptr, v[u]);
-          m = fmaxf(m, magnitude(v[u], odd));
+        for (int u = 0; u < U; ++u) {
+          const int t = min(t0 + u * at_once, n - 1);
+          own[u] = raw8<BF16>(p + t * stride);
+          if (partners) other[u] = raw8<BF16>(p + t * stride + partner);
+        }
+        if (turn_of == 0) __syncthreads();   // the angles are there
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int t = t0 + u * at_once;
+          if (works && t < n) {
+            widen8<BF16>(own[u], v[u]);
+            if (turns) {
+              float o[8];
+              if (partners) widen8<BF16>(other[u], o);
+              turn8(P.rot, d, angles + t * pairs, v[u], o);
+            }
+            m = fmaxf(m, magnitude(v[u], odd));
+          }
+        }
+      } else {
+        if (turn_of == 0) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int t = t0 + u * at_once;
+          if (works && t < n) {
+            new_values<BF16>(P, x + (s.row + t) * P.xs[which].r, d, turns ? angles + t * pairs : nullptr, v[u]);
+            m = fmaxf(m, magnitude(v[u], odd));
+          }
         }
       }
       m = warp_max(m);
@@ -183,15 +276,11 @@ __global__ void __launch_bounds__(AT) lantern_append_kernel(AppendParams P) {
       for (int w = 0; w < AT / 32; ++w) m = fmaxf(m, mine[w]);
       const float scale = new_scale(m, old, s.low > 0, odd);
       const Divider over = divider(scale);
+      uint8_t* to = P.c.row(which, s.page, h, s.low) + d;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = tid + u * AT;
-        if (i < units) {
-          const int t = i / per_row;
-          const uint2 c = make_uint2(encode4(over(v[u][0]), over(v[u][1]), over(v[u][2]), over(v[u][3])),
-                                     encode4(over(v[u][4]), over(v[u][5]), over(v[u][6]), over(v[u][7])));
-          *reinterpret_cast<uint2*>(P.c.row(which, s.page, h, s.low + t) + (i - t * per_row) * 8) = c;
-        }
+        const int t = t0 + u * at_once;
+        if (works && t < n) *reinterpret_cast<uint2*>(to + t * D) = encode8(v[u], over);
       }
       if (s.low > 0 && scale != old) {   // what the block holds is coded anew
         const float ratio = usable_scale(old) ? old / scale : 0.0f;
@@ -245,8 +334,7 @@ __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) 
   for (int t = n - 1; t >= 0; --t) {
     if (t != n - 1) values(t);   // (the last row's are still there)
     if (lane < per_row)
-      *reinterpret_cast<uint2*>(P.c.row(which, s.page, h, s.low + t) + lane * 8) =
-          make_uint2(encode4(over(v[0]), over(v[1]), over(v[2]), over(v[3])), encode4(over(v[4]), over(v[5]), over(v[6]), over(v[7])));
+      *reinterpret_cast<uint2*>(P.c.row(which, s.page, h, s.low + t) + lane * 8) = encode8(v, over);
   }
   if (s.low > 0 && scale != old) {
     const float ratio = usable_scale(old) ? old / scale : 0.0f;
@@ -373,8 +461,8 @@ struct ReadParams {
   const int32_t* counts;
   int32_t* status;
   void* out[2];
-  int R;
-  int64_t units;   // B * R * heads * D / 16
+  int B, R;
+  int units;   // of a sequence: R * heads * D / 16
 };
 
 // A thread per 16 components of a row, keys and values.  Bound by HBM: one byte in, two or four out.
@@ -382,46 +470,47 @@ constexpr int DT = 256;
 template <bool BF16>
 __global__ void __launch_bounds__(DT) lantern_read_kernel(ReadParams P) {
   using T = typename Row<BF16>::T;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * DT + threadIdx.x;
+  const int i = blockIdx.x * DT + threadIdx.x;
   if (i >= P.units) return;
   const int vecs = P.c.D >> 4, per_row = P.c.heads * vecs;
-  const int64_t row = i / per_row;
-  const int rest = static_cast<int>(i - row * per_row), h = rest / vecs, d = (rest - h * vecs) * 16;
-  const int b = static_cast<int>(row / P.R), r = static_cast<int>(row - static_cast<int64_t>(b) * P.R);
+  const int r = i / per_row, rest = i - r * per_row, h = rest / vecs, d = (rest - h * vecs) * 16;
+  for (int b = blockIdx.y; b < P.B; b += gridDim.y) {
   const int first = __ldg(P.first + b), n = P.counts ? __ldg(P.counts + b) : P.R;
   int fault = 0, page = 0;
   const int64_t token = static_cast<int64_t>(first) + r;
   if (first < 0 || n < 0 || n > P.R || static_cast<int64_t>(first) + n > static_cast<int64_t>(P.c.width) * P.c.S) {
     fault = LANTERN_ST_BAD_LENGTH;
   } else if (r >= n) {
-    return;
+    continue;
   } else {
     page = __ldg(P.c.table + static_cast<int64_t>(b) * P.c.width + token / P.c.S);
     if (page < 0 || page >= P.c.pages) fault = LANTERN_ST_BAD_BLOCK;
   }
   if (fault && rest == 0 && P.status) atomicOr(P.status + b, fault);
+  uint4 c[2];
+  float scale[2];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {   // (both reads under way before either is used)
+    c[which] = fault ? make_uint4(0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f, 0x7f7f7f7f)
+                     : *reinterpret_cast<const uint4*>(P.c.row(which, page, h, static_cast<int>(token % P.c.S)) + d);
+    scale[which] = fault ? 1.0f : P.c.scale[which][P.c.block(page, h)];
+  }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float v[16];
-    if (fault) {
+    const uint32_t w[4] = {c[which].x, c[which].y, c[which].z, c[which].w};
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = __int_as_float(0x7fffffff);
-    } else {
-      const uint4 c = *reinterpret_cast<const uint4*>(P.c.row(which, page, h, static_cast<int>(token % P.c.S)) + d);
-      const float scale = P.c.scale[which][P.c.block(page, h)];
-      const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    for (int q = 0; q < 4; ++q) {
+      float x[4];
+      decode4(w[q], x);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float x[4];
-        decode4(w[q], x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e] * scale;
-      }
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e] * scale[which];
     }
-    T* out = static_cast<T*>(P.out[which]) + i * 16;
+    T* out = static_cast<T*>(P.out[which]) + (static_cast<int64_t>(b) * P.units + i) * 16;
     const float lo[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, hi[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
     Row<BF16>::put8(out, lo);
     Row<BF16>::put8(out + 8, hi);
+  }
   }
 }
 
@@ -467,10 +556,12 @@ extern "C" lantern_status lantern_cache_append(const void* k, const void* v, int
     else lantern_append_few_kernel<false><<<grid, FT, 0, st>>>(P);
     e = cudaGetLastError();
   } else {
-    P.heads_per_cta = H < 4 ? H : 4;
-    const dim3 grid((H + P.heads_per_cta - 1) / P.heads_per_cta, static_cast<unsigned>(touched), B);
+    // Heads share a block's angles: as many per CTA as leave eight CTAs per SM, four at most.
+    const int64_t per = static_cast<int64_t>(B) * touched * 2 * H / (8 * 148), most = H < 4 ? H : 4;
+    P.heads_per_cta = static_cast<int>(per < 1 ? 1 : per > most ? most : per);
+    const dim3 grid(2 * ((H + P.heads_per_cta - 1) / P.heads_per_cta), static_cast<unsigned>(touched), B);
     const size_t smem = rotation ? static_cast<size_t>(S) * P.rot.pairs * sizeof(float2) : 0;
-    const int u = (S * D / 8 + AT - 1) / AT;
+    const int at_once = AT / (D / 8), u = (S + at_once - 1) / at_once;   // rows at a time; at most 8 times
     if (u <= 1) e = bf ? launch_append<true, 1>(P, grid, smem, st) : launch_append<false, 1>(P, grid, smem, st);
     else if (u <= 2) e = bf ? launch_append<true, 2>(P, grid, smem, st) : launch_append<false, 2>(P, grid, smem, st);
     else if (u <= 4) e = bf ? launch_append<true, 4>(P, grid, smem, st) : launch_append<false, 4>(P, grid, smem, st);
@@ -503,12 +594,12 @@ extern "C" lantern_status lantern_cache_read(const lantern_cache* cache, const i
   if (B == 0 || R == 0) return LANTERN_OK;
   if (!first || !out_k || !out_v) return LANTERN_E_NULL;
   if ((reinterpret_cast<uintptr_t>(out_k) & 15) || (reinterpret_cast<uintptr_t>(out_v) & 15)) return LANTERN_E_ALIGN;
-  ReadParams P{view_of(cache, table, table_width), first, counts, status, {out_k, out_v}, R,
-               static_cast<int64_t>(B) * R * cache->heads * (cache->head_dim / 16)};
-  const int64_t grid = (P.units + DT - 1) / DT;
-  if (grid > INT32_MAX) return LANTERN_E_SHAPE;
+  const int64_t units = static_cast<int64_t>(R) * cache->heads * (cache->head_dim / 16);
+  if (units > INT32_MAX - DT) return LANTERN_E_SHAPE;
+  ReadParams P{view_of(cache, table, table_width), first, counts, status, {out_k, out_v}, B, R, static_cast<int>(units)};
+  const dim3 grid(static_cast<unsigned>((units + DT - 1) / DT), B < 65535 ? B : 65535);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (dtype == LANTERN_BF16) lantern_read_kernel<true><<<static_cast<unsigned>(grid), DT, 0, st>>>(P);
-  else lantern_read_kernel<false><<<static_cast<unsigned>(grid), DT, 0, st>>>(P);
+  if (dtype == LANTERN_BF16) lantern_read_kernel<true><<<grid, DT, 0, st>>>(P);
+  else lantern_read_kernel<false><<<grid, DT, 0, st>>>(P);
   return cudaGetLastError() == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
 }

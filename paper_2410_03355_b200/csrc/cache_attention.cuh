@@ -23,6 +23,7 @@ struct AttendParams {
   float2* part_ml;    // [unit][split][rows of a unit] maximum (base 2), sum
   int B, R, q_heads, heads, G, S, D, width, pages;
   int row_tiles;      // units per sequence and cache head
+  uint32_t items;     // units * splits
   int splits;         // parts that a unit's tokens are divided into, at most
   int least;          // tiles per part, at least
   int vec;            // query rows may be read 16 bytes at a time
@@ -39,18 +40,29 @@ struct Unit {
   int fault;
   bool rows;             // there are rows to answer
 };
+// What a unit's sequence says of it (read ahead of time where a unit follows another).
+struct UnitIn {
+  int len, n, begin;
+};
+__device__ __forceinline__ int sequence_of(const AttendParams& P, uint32_t unit) {
+  return static_cast<int>(unit / (static_cast<uint32_t>(P.row_tiles) * static_cast<uint32_t>(P.heads)));
+}
+__device__ __forceinline__ UnitIn unit_in(const AttendParams& P, uint32_t unit) {
+  const int b = sequence_of(P, unit);
+  return {__ldg(P.lengths + b), P.counts ? __ldg(P.counts + b) : P.R, P.starts ? max(__ldg(P.starts + b), 0) : 0};
+}
 // (rows of a unit, tokens of a stage)
-__device__ __forceinline__ Unit unit_of(const AttendParams& P, int ROWS, int TILE, int64_t unit, int split) {
+__device__ __forceinline__ Unit unit_of(const AttendParams& P, int ROWS, int TILE, uint32_t unit, int split, const UnitIn& in) {
   Unit u;
   u.split = split;
-  const int mt = static_cast<int>(unit % P.row_tiles);
-  const int64_t bh = unit / P.row_tiles;
-  u.b = static_cast<int>(bh / P.heads);
-  u.h = static_cast<int>(bh - static_cast<int64_t>(u.b) * P.heads);
+  const uint32_t bh = unit / static_cast<uint32_t>(P.row_tiles);
+  const int mt = static_cast<int>(unit - bh * P.row_tiles);
+  u.b = static_cast<int>(bh / static_cast<uint32_t>(P.heads));
+  u.h = static_cast<int>(bh) - u.b * P.heads;
   u.m0 = mt * ROWS;
-  u.len = __ldg(P.lengths + u.b);
-  u.n = P.counts ? __ldg(P.counts + u.b) : P.R;
-  u.begin = P.starts ? max(__ldg(P.starts + u.b), 0) : 0;
+  u.len = in.len;
+  u.n = in.n;
+  u.begin = in.begin;
   u.fault = 0;
   if (u.len < 0 || u.n < 0 || u.n > P.R || static_cast<int64_t>(u.len) + u.n > static_cast<int64_t>(P.width) * P.S) {
     u.fault = LANTERN_ST_BAD_LENGTH;
@@ -69,41 +81,20 @@ __device__ __forceinline__ Unit unit_of(const AttendParams& P, int ROWS, int TIL
   return u;
 }
 
-// Which of the step's rows a row sees, as bits [rows of the unit][words]; false if a parent is out of range.  All threads of the CTA; `nodes` holds R - 1 words.
-__device__ __forceinline__ void ancestor_bits(const AttendParams& P, const Unit& u, int rows, int words, int32_t* nodes, uint32_t* bits, int* fault,
-                                              int tid, int threads) {
-  const int first = u.m0 / P.G;
-  const int32_t* parents = P.parents + static_cast<int64_t>(u.b) * (P.R - 1);
-  for (int i = tid; i < u.n - 1; i += threads) {
-    const int p = __ldg(parents + i);
-    nodes[i] = p;
-    if (p < -1 || p >= i) atomicOr(fault, LANTERN_ST_BAD_PARENT);
-  }
-  for (int i = tid; i < rows * words; i += threads) bits[i] = 0;
-  __syncthreads();
-  if (*fault) return;
-  for (int i = tid; i < rows; i += threads) {
-    int r = first + i;
-    if (r >= u.n) break;
-    uint32_t* mine = bits + i * words;
-    for (; r > 0; r = nodes[r - 1] + 1) mine[r >> 5] |= 1u << (r & 31);
-    mine[0] |= 1u;
-  }
-}
-
 // Joins the parts of a unit: a warp per row, a lane per four components; the weights of up to 32 parts are formed at once, a lane each.
+constexpr int kSms = 148;
 constexpr int kJoinThreads = 128;
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kJoinThreads) lantern_join_kernel(AttendParams P, int ROWS, int TILE) {
   using T = typename Row<BF16>::T;
   constexpr int kPerCta = kJoinThreads / 32;
   const int lane = threadIdx.x & 31;
-  const int64_t unit = blockIdx.x / (ROWS / kPerCta);
+  const uint32_t unit = blockIdx.x / (ROWS / kPerCta);
   const int row = static_cast<int>(blockIdx.x % (ROWS / kPerCta)) * kPerCta + (threadIdx.x >> 5);
-  const Unit u = unit_of(P, ROWS, TILE, unit, 0);
+  const Unit u = unit_of(P, ROWS, TILE, unit, 0, unit_in(P, unit));
   grid_dependency_wait();
   if (!u.rows || u.parts == 1 || row >= u.n * P.G - u.m0) return;
-  const int64_t base = unit * P.splits;
+  const int64_t base = static_cast<int64_t>(unit) * P.splits;
   float M = -INFINITY;
   bool odd = false;
   for (int s = lane; s < u.parts; s += 32) {
@@ -155,7 +146,7 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int 
 // than its products.
 __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity) {
   const uint32_t a = smem_addr(bar);
-  for (uint32_t i = 0; i < (1u << 22); ++i) {
+  for (uint32_t i = 0; i < (1u << 19); ++i) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -169,13 +160,6 @@ __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity) {
   return false;
 }
 
-// What the producer and the warps that multiply share.
-template <int TILE, int STAGES>
-struct StageShared {
-  uint64_t full[STAGES], empty[STAGES];
-  float scale[STAGES][2][TILE / 16];   // of every 16 tokens: keys, values
-  int fault;
-};
 // byte offset of a 16-byte chunk of a token's codes within a stage's keys or values, as the swizzled copy leaves it
 template <int DP>
 __device__ __forceinline__ int chunk_at(int token, int chunk) {
@@ -187,14 +171,14 @@ struct Box {
   float ks, vs;
 };
 template <int TILE>
-__device__ __forceinline__ Box look_up(const AttendParams& P, const Unit& u, int tile, int sub, int stop, int* fault) {
+__device__ __forceinline__ Box look_up(const AttendParams& P, const Unit& u, int tile, int sub, int stop, int& fault) {
   Box x{0, 0, 1.0f, 0.0f};
   const int64_t token = static_cast<int64_t>(u.tile0 + tile) * TILE + sub;
   x.mine = tile < stop && token < u.end && token + min(P.S, TILE) > u.begin;
   if (x.mine) {
     x.page = __ldg(P.table + static_cast<int64_t>(u.b) * P.width + token / P.S);
     if (x.page < 0 || x.page >= P.pages) {
-      atomicOr(fault, LANTERN_ST_BAD_BLOCK);
+      fault |= LANTERN_ST_BAD_BLOCK;
       x.page = 0;
     }
     const int64_t block = static_cast<int64_t>(x.page) * P.heads + u.h;
@@ -202,48 +186,6 @@ __device__ __forceinline__ Box look_up(const AttendParams& P, const Unit& u, int
   }
   return x;
 }
-// The producer warp: tiles [u.lo, stop) of the unit's tokens, keys and values, into the stages, block by block through the table.  A lane per
-// box; the table and the scales are looked up for as many stages as there are lanes, one batch ahead, because a stage's two
-// dependent reads take longer than its copy.
-template <int TILE, int DP, int STAGES>
-__device__ __forceinline__ void produce(const AttendParams& P, const Unit& u, int stop, uint8_t* stages, StageShared<TILE, STAGES>& S, const CUtensorMap* kmap,
-                                        const CUtensorMap* vmap, int lane) {
-  const int sub = min(P.S, TILE), subs = TILE / sub, batch = 32 / subs;   // tokens of a box, boxes of a stage, stages of a batch
-  const int my_stage = lane / subs, my_sub = (lane - my_stage * subs) * sub;
-  Box next = look_up<TILE>(P, u, u.lo + my_stage, my_sub, stop, &S.fault);
-  int it = 0;
-  for (int tile = u.lo; tile < stop; ++tile, ++it) {
-    const int in_batch = it % batch;
-    Box x;
-    if (in_batch == 0) {
-      x = next;
-      next = look_up<TILE>(P, u, tile + batch + my_stage, my_sub, stop, &S.fault);
-    }
-    const int stage = it % STAGES, round = it / STAGES;
-    if (!__all_sync(kFull, round == 0 || await(&S.empty[stage], (round - 1) & 1))) {
-      if (lane == 0) atomicOr(&S.fault, LANTERN_ST_INTERNAL);
-      break;
-    }
-    const bool turn = my_stage == in_batch, mine = turn && x.mine;
-    if (turn)
-      for (int i = 0; i < sub / 16; ++i) {
-        S.scale[stage][0][my_sub / 16 + i] = x.ks;
-        S.scale[stage][1][my_sub / 16 + i] = x.vs;
-      }
-    const int copies = __popc(__ballot_sync(kFull, mine));   // (at least one: every tile has a token that some row sees)
-    if (lane == 0) mbar_expect_tx(&S.full[stage], copies * 2 * sub * DP);
-    __syncwarp();
-    if (mine) {
-      uint8_t* at = stages + (stage * 2 * TILE + my_sub) * DP;
-      const int row = u.h * P.S + ((u.tile0 + tile) * TILE + my_sub) % P.S;
-      tma_load(at, kmap, row, x.page, &S.full[stage]);
-      tma_load(at + TILE * DP, vmap, row, x.page, &S.full[stage]);
-    }
-  }
-  // nothing may be in flight when the CTA ends: the last copies into every stage
-  for (int i = max(0, it - STAGES); i < it; ++i) await(&S.full[i % STAGES], (i / STAGES) & 1);
-}
-
 // Host: how a call's rows and tokens are divided.
 struct Division {
   int rows, tile, DP;    // rows per unit; tokens per stage; padded components
@@ -265,6 +207,10 @@ static cudaError_t launch_join(const AttendParams& P, const Division& d, cudaStr
   return cudaLaunchKernelEx(&cfg, lantern_join_kernel<DP, BF16>, P, d.rows, d.tile);
 }
 
+// Up to 16 rows of a sequence and cache head (cache_attention_few.cu).
+cudaError_t launch_attention_few(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, bool bf16, cudaStream_t st);
+// bf16 queries, up to 64 rows of a sequence and cache head (cache_attention_mid.cu).
+cudaError_t launch_attention_mid(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, cudaStream_t st);
 // More than 16 rows of a sequence and cache head (cache_attention_wide.cu).
 cudaError_t launch_attention_wide(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, bool bf16, cudaStream_t st);
 

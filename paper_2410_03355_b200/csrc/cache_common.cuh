@@ -121,6 +121,25 @@ __device__ __forceinline__ float2 turn(const Rotation& R, int64_t token, int j) 
   sincospif(near, &s, &c);
   return make_float2(__fmaf_rn(-s, rest, c), __fmaf_rn(c, rest, s));
 }
+// The same where many tokens share a pair's frequency: the turns per position as a 64-bit fraction (whole turns dropped), of which a position's
+// multiple modulo one turn is an integer product.  Off by 2^-53 of the turns like the product in double precision.
+__device__ __forceinline__ uint64_t turn_step(const Rotation& R, int j) {
+  const double turns = static_cast<double>(__ldg(R.inv_freq + j)) * 0.15915494309189533577;
+  return __double2ull_rn((turns - floor(turns)) * 18446744073709551616.0);   // (2^64 saturates: 2^-64 of a turn short)
+}
+__device__ __forceinline__ float2 turn_by(uint64_t step, int position) {
+  const int halves = static_cast<int>(static_cast<uint32_t>((step * static_cast<uint64_t>(static_cast<int64_t>(position))) >> 32));   // in 2^-31 half turns
+  const float near = static_cast<float>(halves);
+  const float rest = static_cast<float>(static_cast<int>(static_cast<int64_t>(halves) - static_cast<int64_t>(near))) * (3.14159265f * 4.656612873e-10f);
+  float s, c;
+  sincospif(near * 4.656612873e-10f, &s, &c);
+  return make_float2(__fmaf_rn(-s, rest, c), __fmaf_rn(c, rest, s));
+}
+__device__ __forceinline__ int position_of(const Rotation& R, int64_t token, int j) {
+  const int axis = (j >= R.ends[0]) + (j >= R.ends[1]) + (j >= R.ends[2]);
+  return __ldg(R.positions + axis * R.plane + token);
+}
+
 // The two components of a turned pair, each with one fused rounding and one of the product, so that every kernel and path gives the same bits.
 __device__ __forceinline__ float turned_low(float a, float b, float2 cs) { return __fmaf_rn(a, cs.x, -__fmul_rn(b, cs.y)); }
 __device__ __forceinline__ float turned_high(float a, float b, float2 cs) { return __fmaf_rn(b, cs.x, __fmul_rn(a, cs.y)); }
