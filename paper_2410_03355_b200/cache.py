@@ -46,12 +46,6 @@ def declare(lib):
     return operators
 
 
-def _native(stream):
-    """The native part of the binding for a call on the current stream, or None."""
-    load_library()
-    return binding._call if stream is None else None
-
-
 def _dtype(t: torch.Tensor, name: str) -> int:
     if t.dtype == torch.bfloat16:
         return BF16
@@ -149,14 +143,15 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, rotation: Rotation, *, inve
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_rotary: rows x [B, R, H, D] turned by positions [axes, B, R].  inverse=True turns back, which is also the gradient with
     respect to x of a gradient with respect to the result.  out: a tensor like x, or x itself; allocated if not given."""
-    lib, call = load_library(), _native(stream)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if call is not None and rotation is not None:
-        rc = call.rotary(x, positions, rotation._at, rotation._device, inverse, out)
+    if binding._call is not None and stream is None and rotation is not None:   # (loaded: the native part)
+        rc = binding._call.rotary(x, positions, rotation._at, rotation._device, inverse, out)
         if rc is not None:
-            _check(rc, "lantern_rotary")
+            if rc != 0:
+                raise LanternError(rc, "lantern_rotary")
             return out
+    lib = load_library()
     px, xs = _rows(x, "x")
     dtype = _dtype(x, "x")
     if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
@@ -185,12 +180,12 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, table: torch.
     """lantern_cache_append: rows k, v [B, R, heads, D] become tokens lengths[b], lengths[b] + 1, ... of their sequences; keys are turned by
     positions [axes, B, R] on the way if a rotation is given.  table [B, blocks], lengths [B], counts [B] (rows that there are; None = R)
     and status [B] (fault bits are OR-ed into it) are int32."""
-    lib, call = load_library(), _native(stream)
-    if call is not None:
-        rc = call.append(k, v, cache._at, cache._device, table, lengths, counts, positions, None if rotation is None else rotation._at,
-                         None if rotation is None else rotation._device, status)
+    if binding._call is not None and stream is None:
+        rc = binding._call.append(k, v, cache._at, cache._device, table, lengths, counts, positions, None if rotation is None else rotation._at,
+                                  None if rotation is None else rotation._device, status)
         if rc is not None:
             return _check(rc, "lantern_cache_append")
+    lib = load_library()
     pk, ks = _rows(k, "k")
     pv, vs = _rows(v, "v")
     dtype = _dtype(k, "k")
@@ -224,12 +219,13 @@ def cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, length
     """lantern_cache_attention: queries [B, R, q_heads, D] of the rows that cache_append() has just put behind the sequences' `lengths`
     tokens, attending to the tokens from starts[b] (None: 0) on and to their own ancestors (tree_parents [B, R-1] as in verify(); None =
     a chain, i.e. causal).  scale: None = head_dim ** -0.5.  Rows that `counts` leaves out stay as they are in `out`."""
-    lib, call = load_library(), _native(stream)
-    if call is not None and out is not None and workspace is not None:
-        rc = call.attention(q, cache._at, cache._device, table, lengths, counts, starts, tree_parents, scale, out, workspace, status)
+    if binding._call is not None and stream is None and out is not None and workspace is not None:
+        rc = binding._call.attention(q, cache._at, cache._device, table, lengths, counts, starts, tree_parents, scale, out, workspace, status)
         if rc is not None:
-            _check(rc, "lantern_cache_attention")
+            if rc != 0:
+                raise LanternError(rc, "lantern_cache_attention")
             return out
+    lib = load_library()
     pq, qs = _rows(q, "q")
     dtype = _dtype(q, "q")
     B, R, HQ, D = q.shape
@@ -268,14 +264,15 @@ def cache_keep(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, accep
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_cache_keep: after verify(), moves the accepted path's tokens behind the root's and returns the sequences' new lengths (the
     root's and the path's tokens counted).  accept_len [B], accept_path [B, N] as verify() gives them."""
-    lib, call = load_library(), _native(stream)
     if out_lengths is None:
         out_lengths = torch.empty_like(lengths)
-    if call is not None:
-        rc = call.keep(cache._at, cache._device, table, lengths, accept_len, accept_path, out_lengths, status)
+    if binding._call is not None and stream is None:
+        rc = binding._call.keep(cache._at, cache._device, table, lengths, accept_len, accept_path, out_lengths, status)
         if rc is not None:
-            _check(rc, "lantern_cache_keep")
+            if rc != 0:
+                raise LanternError(rc, "lantern_cache_keep")
             return out_lengths
+    lib = load_library()
     if accept_path.dim() != 2:
         raise ValueError("accept_path must be [B, N]")
     B, N = accept_path.shape
@@ -294,12 +291,13 @@ def cache_read(cache: KVCache, table: torch.Tensor, first: torch.Tensor, rows: i
                stream: Optional[torch.cuda.Stream] = None):
     """lantern_cache_read: the keys and values [B, rows, heads, D] of tokens first[b], first[b] + 1, ... in bf16 or fp32 (out: a pair of
     such tensors).  Rows that `counts` leaves out stay as they are in `out`."""
-    lib, call = load_library(), _native(stream)
-    if call is not None and out is not None:
-        rc = call.read(cache._at, cache._device, table, first, rows, counts, *out, status)
+    if binding._call is not None and stream is None and out is not None:
+        rc = binding._call.read(cache._at, cache._device, table, first, rows, counts, *out, status)
         if rc is not None:
-            _check(rc, "lantern_cache_read")
+            if rc != 0:
+                raise LanternError(rc, "lantern_cache_read")
             return out
+    lib = load_library()
     B, rows = int(table.shape[0]), int(rows)
     dev = cache.device
     shape = (B, rows, cache.heads, cache.head_dim)

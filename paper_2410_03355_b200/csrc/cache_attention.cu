@@ -1,5 +1,5 @@
-// Attention of a step's rows to the paged 8-bit cache: the call.  Up to 16 rows of a sequence and cache head go to cache_attention_few.cu, up to 64 bf16 ones to
-// cache_attention_mid.cu, all others to cache_attention_wide.cu.
+// Attention of a step's rows to the paged 8-bit cache: the call.  The kernels are in cache_attention_few.cu, _mid.cu and _wide.cu, by the number of
+// rows of a sequence and cache head.
 #include "cache_attention.cuh"
 
 namespace lantern {
@@ -31,23 +31,29 @@ lantern_status code_map(CUtensorMap* map, const void* code, const lantern_cache*
              : LANTERN_E_CUDA;
 }
 
+// Which kernel takes a call, and how its rows and tokens are divided.
+//   Up to 16 rows: `few` (128 single tokens of 4 heads a group over 2300: 112 us; 16 rows of 64 in the form of `mid` 193).
+//   Up to 64 bf16 rows: `mid`; with more than 64 components and contexts that can be long, `wide` (64 trees of 61 rows, 20 heads, 128 components:
+//   650 tokens mid 196 us, wide 220; 2250 tokens mid 572, wide 435; 64 components: mid 107 and 284, wide 158 and 346).
+//   More rows, and fp32 ones from 17 on: `wide` (16 trees of 61 rows, 8 heads a group: 102 us, in 64 rows at a time as mid takes them 135).
 static Division divide(int dtype, int B, int R, int q_heads, const lantern_cache* c, int width) {
   Division d;
-  const int64_t G = q_heads / c->heads, M = G * R;
+  const int64_t G = q_heads / c->heads, M = G * R, room = static_cast<int64_t>(width) * c->page_tokens;
   d.DP = c->head_dim <= 64 ? 64 : 128;
   d.rows = M <= 16 ? 16 : M <= 64 ? 64 : 128;
-  d.tile = d.rows == 16 ? 32 : d.DP == 64 ? 64 : d.rows == 64 && dtype == LANTERN_BF16 ? 32 : 128;   // (as the kernels have it)
+  d.kernel = d.rows == 16 ? Division::kFew : d.rows == 64 && dtype == LANTERN_BF16 && (d.DP == 64 || room < 2048) ? Division::kMid : Division::kWide;
+  d.tile = d.kernel == Division::kFew ? 32 : d.DP == 64 ? 64 : d.kernel == Division::kMid ? 32 : 128;   // (as the kernels have it)
   d.row_tiles = static_cast<int>((M + d.rows - 1) / d.rows);
   d.units = static_cast<int64_t>(B) * c->heads * d.row_tiles;
-  const int64_t tiles = (static_cast<int64_t>(width) * c->page_tokens + d.tile - 1) / d.tile;
-  const bool persistent = d.rows > 16 && !(d.rows == 64 && dtype == LANTERN_BF16);
-  // Places for CTAs on the GPU; a unit is divided where there are fewer units than places: into as many parts as fill the places once where
-  // CTAs are persistent (a part's start and end cost as much as several tiles), else twice.
-  const int64_t slots = kSms * (persistent ? (d.DP == 64 ? 2 : 1) : d.rows == 64 ? (d.DP == 64 ? 4 : 3) : 2);
-  const int64_t units = d.units > 0 ? d.units : 1;
-  int64_t splits = units >= slots ? 1 : persistent ? slots / units : (2 * slots + units - 1) / units;
-  d.least = 2;
-  if (splits > tiles / d.least) splits = tiles / d.least;
+  // A unit is divided where there are fewer units than places for CTAs on the GPU: into as many parts as fill the places once where CTAs are
+  // persistent (`wide`: a part's start and end cost as much as several tiles), else twice; a part has 512 tokens at least, so that a short
+  // context is one launch.
+  const int64_t tiles = (room + d.tile - 1) / d.tile, units = d.units > 0 ? d.units : 1;
+  const int64_t places = kSms * (d.kernel == Division::kWide ? (d.DP == 64 ? 2 : 1) : d.kernel == Division::kFew || d.DP == 64 ? 3 : 2);
+  d.least = 512 / d.tile;
+  int64_t splits = units >= places ? 1 : d.kernel == Division::kWide ? places / units : (2 * places + units - 1) / units;
+  const int64_t most = (tiles + d.least - 1) / d.least;
+  if (splits > most) splits = most;
   d.splits = static_cast<int>(splits < 1 ? 1 : splits > 512 ? 512 : splits);
   return d;
 }
@@ -124,8 +130,8 @@ extern "C" lantern_status lantern_cache_attention(const void* q, void* out, int 
   if ((bad = code_map(&km, cache->k_code, cache, d.DP, tokens)) != LANTERN_OK || (bad = code_map(&vm, cache->v_code, cache, d.DP, tokens)) != LANTERN_OK) return bad;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (d.rows == 16) e = launch_attention_few(P, km, vm, d, bf, st);
-  else if (d.rows == 64 && bf) e = launch_attention_mid(P, km, vm, d, st);
+  if (d.kernel == Division::kFew) e = launch_attention_few(P, km, vm, d, bf, st);
+  else if (d.kernel == Division::kMid) e = launch_attention_mid(P, km, vm, d, st);
   else e = launch_attention_wide(P, km, vm, d, bf, st);
   return e == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
 }

@@ -188,6 +188,7 @@ __device__ __forceinline__ Box look_up(const AttendParams& P, const Unit& u, int
 }
 // Host: how a call's rows and tokens are divided.
 struct Division {
+  enum { kFew, kMid, kWide } kernel;
   int rows, tile, DP;    // rows per unit; tokens per stage; padded components
   int row_tiles, splits, least;
   int64_t units;

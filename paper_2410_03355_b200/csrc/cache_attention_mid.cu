@@ -58,7 +58,7 @@ __device__ __forceinline__ int half_at(int token, int unit) {
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 3) lantern_attention_mid_kernel(AttendParams P, const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_mid_kernel(AttendParams P, const __grid_constant__ CUtensorMap kmap,
                                                                                        const __grid_constant__ CUtensorMap vmap) {
   using T = __nv_bfloat16;
   constexpr int KS = DP / 16, NT = DP / 8;             // steps of the scores' products, column tiles of the output
@@ -319,19 +319,19 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 3) lantern_attention_
         const float a = max3(max3(c[2 * k][2 * half], c[2 * k][2 * half + 1], c[2 * k + 1][2 * half]), c[2 * k + 1][2 * half + 1], -INFINITY);
         m = fmaxf(m, a * f[half][k]);
       }
-      m = fmaxf(m, __shfl_xor_sync(kFull, m, 1));
-      m = fmaxf(m, __shfl_xor_sync(kFull, m, 2));
-      most[half] = m;
+      most[half] = m;   // of this lane's tokens
       grow |= m > ref[half] + 8.0f;
     }
     // The maximum that the numerators refer to follows the running maximum only when it has fallen behind by 2^8 (the reference scale of the
-    // values: 2^5), so that the accumulators are rarely touched; a numerator stays below 2^8 * 2^5, a half's largest value is 2^16.
+    // values: 2^5), so that the accumulators are rarely touched -- and the lanes' maxima rarely put together; a numerator stays below 2^8 * 2^5, a
+    // half's largest value is 2^16.
     if (__any_sync(kFull, grow)) {
       const float v_new = fmaxf(vref, v_most), v_ratio = v_new > 0.0f ? vref / v_new : 0.0f;
       float w[2];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const float m = fmaxf(ref[half], most[half]);
+        float m = fmaxf(most[half], __shfl_xor_sync(kFull, most[half], 1));
+        m = fmaxf(ref[half], fmaxf(m, __shfl_xor_sync(kFull, m, 2)));
         const float k = ref[half] == -INFINITY ? 0.0f : ex2_approx(ref[half] - m);
         ref[half] = m;
         sum[half] *= k;
