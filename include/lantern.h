@@ -409,7 +409,8 @@ lantern_status lantern_rotary(const void* x, void* out, int dtype, int B, int R,
  * A NaN or infinite value is stored as the NaN code, sets LANTERN_ST_NONFINITE and does not count for the scale.
  * With LANTERN_ST_BAD_LENGTH nothing of the sequence is written, with LANTERN_ST_BAD_BLOCK nothing of the block.
  *
- *   k, v          [B, R, heads, D], strides in elements (batch, row, head); heads and D are the cache's */
+ *   k, v          [B, R, heads, D], strides in elements (batch, row, head); heads and D are the cache's; B <= 65535,
+ *                 R <= 65534 * page_tokens */
 lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int B, int R, const int64_t k_stride[3],
                                     const int64_t v_stride[3], const lantern_cache* cache, const int32_t* table,
                                     int table_width, const int32_t* lengths, const int32_t* counts,
@@ -423,14 +424,15 @@ lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int
  * components concerned, and no other row.  A sequence with a fault (BAD_LENGTH, BAD_BLOCK, BAD_PARENT among its rows)
  * gives NaN in rows that the fault concerns.
  *
- * Scores, the softmax's maximum and sum and the outputs are fp32; queries enter the products exactly with bf16 and to 22
- * bits with fp32, probabilities to 11 bits with bf16 (half a bit of which the output's own 8 bits show) and to 22 with fp32.
+ * Scores, the softmax's maximum and sum and the outputs are fp32.  Queries enter the products as halves relative to the
+ * row's largest component (bf16: exactly, but for components 2^28 times smaller than it; fp32: as two halves, 22 bits);
+ * probabilities, relative to the row's largest, as halves (11 bits) with bf16 and as two halves with fp32.
  *
  *   q             [B, R, q_heads, D], strides in elements; 16-byte aligned rows are fastest, any alignment is served
- *   out           [B, R, q_heads, D] contiguous, dtype of q
+ *   out           [B, R, q_heads, D] contiguous, dtype of q, 16-byte aligned; must not overlap q (out == q: LANTERN_E_PARAM)
  *   q_heads       a multiple of the cache's heads
  *   tree_parents  [B, R-1] int32, R <= 1025; NULL = chain, any R
- *   starts        [B] int32, NULL = 0 (tokens ahead of starts[b] are padding and are not read)
+ *   starts        [B] int32, NULL = 0 (tokens ahead of starts[b] are padding and count for nothing; negative: 0)
  *   scale         finite
  *   workspace     lantern_cache_attention_workspace_bytes(...) bytes, 256-byte aligned; NULL if that is 0 */
 size_t lantern_cache_attention_workspace_bytes(int dtype, int B, int R, int q_heads, const lantern_cache* cache,
@@ -447,8 +449,8 @@ lantern_status lantern_cache_attention(const void* q, void* out, int dtype, int 
  * out_lengths[b] = lengths[b] + 1 + n.  Tokens behind are undefined.  Where a token moves into a block of a smaller
  * scale, that block takes the larger one and its tokens are coded anew.
  * A fault (BAD_PATH, BAD_LENGTH, BAD_BLOCK) leaves the sequence as it is, with out_lengths[b] = lengths[b].
- *   accept_len    [B], accept_path [B, N] as lantern_verify writes them; 0 <= N <= 1024
- *   out_lengths   [B], must not overlap lengths */
+ *   accept_len    [B], accept_path [B, N] as lantern_verify writes them; B <= 65535, 0 <= N <= 1024
+ *   out_lengths   [B], must not overlap lengths (out_lengths == lengths: LANTERN_E_PARAM) */
 lantern_status lantern_cache_keep(const lantern_cache* cache, const int32_t* table, int table_width,
                                   const int32_t* lengths, const int32_t* accept_len, const int32_t* accept_path, int B,
                                   int N, int32_t* out_lengths, int32_t* status, void* cuda_stream);

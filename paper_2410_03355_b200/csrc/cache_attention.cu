@@ -89,6 +89,7 @@ extern "C" lantern_status lantern_cache_attention(const void* q, void* out, int 
   if (!isfinite(scale)) return LANTERN_E_PARAM;
   if (B == 0 || R == 0) return LANTERN_OK;
   if (!q || !out || !q_stride || !lengths) return LANTERN_E_NULL;
+  if (q == out) return LANTERN_E_PARAM;
   const bool bf = dtype == LANTERN_BF16;
   const int size = bf ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(q) % size || (reinterpret_cast<uintptr_t>(out) & 15)) return LANTERN_E_ALIGN;

@@ -96,11 +96,6 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
       next = look_up<kTile>(P, u, u.lo + i + batch + my_tile, my_sub, u.hi, found);
     }
     const bool turn = my_tile == in_batch, mine = turn && box.mine;
-    if (turn)
-      for (int e = 0; e < sub / 16; ++e) {
-        S.scale[i & 3][0][my_sub / 16 + e] = box.ks;
-        S.scale[i & 3][1][my_sub / 16 + e] = box.vs;
-      }
     const int copies = __popc(__ballot_sync(kFull, mine));   // (at least one: every tile has a token that some row sees)
     if (lane == 0) mbar_expect_tx(&S.full[stage], copies * 2 * sub * DP);
     __syncwarp();
@@ -110,6 +105,11 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
       tma_load(at, &kmap, row, box.page, &S.full[stage]);
       tma_load(at + kTile * DP, &vmap, row, box.page, &S.full[stage]);
     }
+    if (turn)   // (read behind a barrier of the block, not behind the copies)
+      for (int e = 0; e < sub / 16; ++e) {
+        S.scale[i & 3][0][my_sub / 16 + e] = box.ks;
+        S.scale[i & 3][1][my_sub / 16 + e] = box.vs;
+      }
   };
   if (warp == 0)
     for (int i = 0; i < min(tiles, kStages); ++i) ask(i);

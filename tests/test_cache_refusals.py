@@ -32,13 +32,13 @@ def append(c=None, k=AT, v=AT, dtype=lt.BF16, B=2, R=3, ks=None, vs=None, table=
     return lt.load_library().lantern_cache_append(k, v, dtype, B, R, ks, vs, ref(c), table, width, lengths, None, ref(rot), None, None)
 
 
-def attention(c=None, q=AT, out=AT, dtype=lt.BF16, B=2, R=3, HQ=8, table=AT, width=4, lengths=AT, parents=None, scale=0.1, ws=None, ws_bytes=0):
+def attention(c=None, q=AT, out=AT + 4096, dtype=lt.BF16, B=2, R=3, HQ=8, table=AT, width=4, lengths=AT, parents=None, scale=0.1, ws=None, ws_bytes=0):
     c = c or cache()
     return lt.load_library().lantern_cache_attention(q, out, dtype, B, R, HQ, strides(), ref(c), table, width, lengths, None, None, parents, scale, None,
                                                   ws, ws_bytes, None)
 
 
-def keep(c=None, table=AT, width=4, lengths=AT, accept=AT, path=AT, B=2, N=3, out=AT):
+def keep(c=None, table=AT, width=4, lengths=AT, accept=AT, path=AT, B=2, N=3, out=AT + 4096):
     c = c or cache()
     return lt.load_library().lantern_cache_keep(ref(c), table, width, lengths, accept, path, B, N, out, None, None)
 
@@ -85,6 +85,7 @@ def test_attention():
     assert attention(HQ=0) == SHAPE and attention(HQ=6) == SHAPE
     assert attention(R=1026, parents=AT) == SHAPE
     assert attention(scale=float("nan")) == PARAM and attention(scale=float("inf")) == PARAM
+    assert attention(out=AT) == PARAM                  # in place
     assert attention(out=AT + 8) == ALIGN and attention(q=AT + 1) == ALIGN
     assert attention(B=1 << 16, R=1 << 16) == SHAPE
     long = dict(B=1, R=1, width=1000)
@@ -106,6 +107,7 @@ def _view():
 def test_keep():
     assert keep(lengths=None) == NULL and keep(accept=None) == NULL and keep(path=None) == NULL and keep(out=None) == NULL
     assert keep(N=-1) == SHAPE and keep(N=1025) == SHAPE and keep(B=65536) == SHAPE
+    assert keep(out=AT) == PARAM                       # in place
     assert keep(B=0) == 0
 
 

@@ -448,6 +448,19 @@ def test_attention_strided_queries(R, G, dtype):
     assert torch.equal(lt.cache_attention(turned, cache, table, i32(lengths)), got)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D,R,tree", [(32, 70, 4), (96, 70, 0), (80, 35, 3)])
+def test_attention_more_units_than_places(D, R, tree, dtype):
+    """More rows and heads than the GPU takes at once, sequences of all lengths, some without rows, some that see nothing."""
+    g = gen(62)
+    B = 50
+    lengths = torch.randint(0, 150, (B,), generator=g).tolist()
+    counts = torch.randint(0, R + 1, (B,), generator=g).tolist()
+    starts = torch.randint(0, 200, (B,), generator=g).tolist()
+    lengths[3], counts[5], counts[6], starts[7] = 0, 0, R, 0
+    run_attention(lengths, R, 7, 1, D, 16, dtype, tree=tree, counts=counts, starts=starts)
+
+
 def test_attention_largest_tree():
     run_attention([70], 1025, 1, 1, 16, 64, BF, tree=100)
 
