@@ -302,11 +302,11 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         }
         tmem_fence_after();
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s)
+        for (int q = TERMS - 1; q >= 0; --q)   // (the small terms first: every addition to the large ones costs a rounding)
 #pragma unroll
-          for (int q = 0; q < TERMS; ++q)
+          for (int s = 0; s < DP / 16; ++s)
             multiply(tmem + C::kScores + k * TILE, tmem + C::kQuery + q * (DP / 2) + s * 8,
-                     halves_at(base + k * 2 * C::kHalves + (s >> 2) * RUN + (s & 3) * 32, RUN), product(TILE, false), s + q > 0);
+                     halves_at(base + k * 2 * C::kHalves + (s >> 2) * RUN + (s & 3) * 32, RUN), product(TILE, false), s > 0 || q < TERMS - 1);
         commit(&S.scores_full[k]);
         commit(&S.keys_free[k]);
         mbar_arrive(&S.scores_full[k]);   // (what the converting warps wrote beside the keys is ordered by this arrival)
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       for (int which = 0; which < 2; ++which) {
         if (n >= 2) ok = ok && await(which ? &S.values_free[k] : &S.keys_free[k], ((n >> 1) - 1) & 1);
         uint8_t* out = halves + (k * 2 + which) * C::kHalves;
-#pragma unroll
+#pragma unroll 2
         for (int c = 0; c < CHUNKS; ++c) {
           uint4 x = *reinterpret_cast<const uint4*>(raw + which * TILE * DP + (code_from ^ (c << 4)));
           if (which == 1 && edge) {   // where a token may be hidden from a row its NaN must not reach the row through a zero probability
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       };
       float most = 0.0f;
       bool odd = false;
-#pragma unroll
+#pragma unroll 1
       for (int run = 0; run < RUNS; ++run) {
         fetch(run);
 #pragma unroll
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       float mult = most == 0.0f || odd || P.scale_log2 == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(up) << 23);
       if (P.scale_log2 < 0.0f) mult = -mult;
       factor = odd ? __int_as_float(0x7fffffff) : ldexpf(fabsf(P.scale_log2), 127 - up);
-#pragma unroll
+#pragma unroll 1
       for (int run = 0; run < RUNS; ++run) {
         if (RUNS > 1) fetch(run);
         constexpr int WORDS = 64 / sizeof(T);   // of halves in a run: 32 or 16
@@ -556,60 +556,58 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         ok = await(&S.scores_full[k], (n >> 1) & 1);
         const int token0 = (u.tile0 + u.lo + i) * TILE;
         const bool edge = S.tile_flags[n & 3] & kEdge;
-        uint32_t see[MINE], nan[MINE];
-        if (edge) {
-          ok = ok && await(&S.values_full[k], (n >> 1) & 1);
-#pragma unroll
-          for (int j = 0; j < MINE; ++j) {
-            const int c = c0 + j, a = token0 + 32 * c, ahead = a - u.len;
-            nan[j] = TILE == 64 ? S.bad[n & 3][c] | S.bad[n & 3][c + 2] : S.bad[n & 3][c];
-            uint32_t x = low_bits(-ahead + (P.parents ? 0 : r + 1));
-            if (P.parents) {
-              if (ahead >= 0) {
-                const int w = ahead >> 5;
-                const uint32_t lo = w < words ? seen[w] : 0u, hi = w + 1 < words ? seen[w + 1] : 0u;
-                x |= __funnelshift_r(lo, hi, ahead & 31);
-              } else if (ahead > -32) {
-                x |= seen[0] << -ahead;
-              }
-            }
-            x &= ~low_bits(u.begin - a);
-            see[j] = there ? x : 0u;
-          }
-        }
+        if (edge) ok = ok && await(&S.values_full[k], (n >> 1) & 1);
         __syncwarp();
         tmem_fence_after();
-        float f[2 * MINE];
-#pragma unroll
-        for (int c = 0; c < 2 * MINE; ++c) {
-          f[c] = f0 * S.key_scale[n & 3][2 * c0 + c];
-          if (f[c] < 1.17549435e-38f) f[c] = 1.17549435e-38f;   // (not zero: a hidden token stays at minus infinity)
-        }
+        auto factors = [&](int j, float& fa, float& fb) {   // of the two sixteens of run j of this thread's
+          fa = f0 * S.key_scale[n & 3][2 * (c0 + j)], fb = f0 * S.key_scale[n & 3][2 * (c0 + j) + 1];
+          if (fa < 1.17549435e-38f) fa = 1.17549435e-38f;   // (not zero: a hidden token stays at minus infinity)
+          if (fb < 1.17549435e-38f) fb = 1.17549435e-38f;
+        };
+        auto visible = [&](int j, uint32_t& see, uint32_t& nan) {   // tokens of run j that the row sees, and those of them with a NaN among their values
+          const int c = c0 + j, a = token0 + 32 * c, ahead = a - u.len;
+          see = low_bits(-ahead + (P.parents ? 0 : r + 1));
+          if (P.parents) {
+            if (ahead >= 0) {
+              const int w = ahead >> 5;
+              const uint32_t lo = w < words ? seen[w] : 0u, hi = w + 1 < words ? seen[w + 1] : 0u;
+              see |= __funnelshift_r(lo, hi, ahead & 31);
+            } else if (ahead > -32) {
+              see |= seen[0] << -ahead;
+            }
+          }
+          see &= ~low_bits(u.begin - a);
+          if (!there) see = 0u;
+          nan = see & (TILE == 64 ? S.bad[n & 3][c] | S.bad[n & 3][c + 2] : S.bad[n & 3][c]);
+        };
         const uint32_t scores = lanes + C::kScores + k * TILE;
         float top = -INFINITY;
         uint32_t x[KEEP ? MINE : 1][32];   // the scores, if there are registers for them
         auto get = [&](int j, uint32_t (&y)[32]) {   // run j of this thread's, hidden tokens at minus infinity
           tmem_ld32(y, scores + 32 * (c0 + j));
           if (edge) {
-            const uint32_t s = see[j], bad = nan[j];
+            uint32_t see, nan;
+            visible(j, see, nan);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              y[e] = (s >> e) & 1u ? y[e] : 0xff800000u;
-              if ((s & bad) >> e & 1u) y[e] = 0x7fffffffu;
+              y[e] = (see >> e) & 1u ? y[e] : 0xff800000u;
+              if ((nan >> e) & 1u) y[e] = 0x7fffffffu;
             }
           }
         };
-#pragma unroll
+        constexpr int UNROLL = KEEP ? MINE : 1;   // (code that does not fit the instruction cache costs more than a loop)
+#pragma unroll UNROLL
         for (int j = 0; j < MINE; ++j) {
           uint32_t(&y)[32] = x[KEEP ? j : 0];
           get(j, y);
-          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, fa, fb;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             a[0] = fmaxf(a[0], __uint_as_float(y[e])), a[1] = fmaxf(a[1], __uint_as_float(y[8 + e]));
             a[2] = fmaxf(a[2], __uint_as_float(y[16 + e])), a[3] = fmaxf(a[3], __uint_as_float(y[24 + e]));
           }
-          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]) * f[2 * j], fmaxf(a[2], a[3]) * f[2 * j + 1]));
+          factors(j, fa, fb);
+          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]) * fa, fmaxf(a[2], a[3]) * fb));
         }
         // The maximum that the probabilities refer to follows the running maximum only when it has fallen behind by 2^8 (a half holds 2^16), so
         // that the accumulators are rarely touched.
@@ -621,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
             ok = ok && await(&S.values_free[(n - 1) & 1], ((n - 1) >> 1) & 1);
             __syncwarp();
             tmem_fence_after();
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
               uint32_t x[32];
               tmem_ld32(x, lanes + C::kOutput + 32 * c);
@@ -634,14 +632,16 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         const float base = ref == -INFINITY ? 0.0f : ref;
         uint64_t part[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
         const uint64_t back = pack2(-base, -base);
-#pragma unroll
+#pragma unroll UNROLL
         for (int j = 0; j < MINE; ++j) {
           uint32_t(&y)[32] = x[KEEP ? j : 0];
           if (!KEEP) get(j, y);
           uint32_t h[16], l[16];
+          float fa, fb;
+          factors(j, fa, fb);
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float ff = f[2 * j + (e >> 4)];
+            const float ff = e < 16 ? fa : fb;
             float a, b;
             unpack2(fma2(pack2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), pack2(ff, ff), back), a, b);
             a = ex2_approx(a), b = ex2_approx(b);
