@@ -32,16 +32,17 @@ lantern_status code_map(CUtensorMap* map, const void* code, const lantern_cache*
 }
 
 // Which kernel takes a call, and how its rows and tokens are divided.
-//   Up to 16 rows: `few` (128 single tokens of 4 heads a group over 2300: 112 us; 16 rows of 64 in the form of `mid` 193).
-//   Up to 64 bf16 rows: `mid`; with more than 64 components and contexts that can be long, `wide` (64 trees of 61 rows, 20 heads, 128 components:
-//   650 tokens mid 196 us, wide 220; 2250 tokens mid 572, wide 435; 64 components: mid 107 and 284, wide 158 and 346).
-//   More rows, and fp32 ones from 17 on: `wide` (16 trees of 61 rows, 8 heads a group: 102 us, in 64 rows at a time as mid takes them 135).
+//   Up to 16 rows: `few` (128 single tokens of 4 heads a group over 2300 tokens: 112 us; as 64 rows mostly empty, 193).
+//   Up to 64 bf16 rows: `mid` where contexts are short, `wide` where they can be long enough for its units' longer start and end (trees of 61 rows, 20
+//   heads; 256 of 64 components over 650 tokens: mid 362 us, wide 400; 64 of them over 2250: 283 and 244; 64 of 128 components over 340 tokens: 138
+//   and 142, over 650: 197 and 181).  `room` is what the table can hold, about twice these averages.
+//   More rows, and fp32 ones from 17 on: `wide` (16 trees of 61 rows, 8 heads a group, 1200 tokens: 76 us, in 64 rows at a time as mid takes them 135).
 static Division divide(int dtype, int B, int R, int q_heads, const lantern_cache* c, int width) {
   Division d;
   const int64_t G = q_heads / c->heads, M = G * R, room = static_cast<int64_t>(width) * c->page_tokens;
   d.DP = c->head_dim <= 64 ? 64 : 128;
   d.rows = M <= 16 ? 16 : M <= 64 ? 64 : 128;
-  d.kernel = d.rows == 16 ? Division::kFew : d.rows == 64 && dtype == LANTERN_BF16 && (d.DP == 64 || room < 2048) ? Division::kMid : Division::kWide;
+  d.kernel = d.rows == 16 ? Division::kFew : d.rows == 64 && dtype == LANTERN_BF16 && room < (d.DP == 64 ? 2048 : 1024) ? Division::kMid : Division::kWide;
   d.tile = d.kernel == Division::kFew ? 32 : d.DP == 64 ? 64 : d.kernel == Division::kMid ? 32 : 128;   // (as the kernels have it)
   d.row_tiles = static_cast<int>((M + d.rows - 1) / d.rows);
   d.units = static_cast<int64_t>(B) * c->heads * d.row_tiles;

@@ -36,7 +36,7 @@ struct Shape {
 
 enum { kFirst = 1, kLast = 2, kEnd = 4, kEdge = 8 };   // of a tile: of its unit; there are no more; some row may not see all of its tokens
 
-constexpr int kJoinRow = 65;
+constexpr int kJoinRow = 68;   // (rows 16 bytes apart in the banks)
 constexpr int kSlots = 8;   // units that can be under way: one per tile in the stages, in the halves and in the scores, at most
 template <int DP>
 struct WideShared {
@@ -51,7 +51,7 @@ struct WideShared {
   float vref[kSlots];
   int fault[kSlots];                     // of a unit, found by the producer
   float2 ml[64];
-  uint32_t tmem;
+  alignas(16) uint32_t tmem;   // (what follows in shared memory starts on 16 bytes)
 };
 
 // ---- tensor memory and products -----------------------------------------------------------------------------------------
@@ -704,7 +704,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
           if (d0 > 0) rows_sync();
           if (group == 1)
 #pragma unroll
-            for (int e = 0; e < 64; ++e) join[row][e] = __uint_as_float(y[e >> 5][e & 31]);
+            for (int e = 0; e < 64; e += 4)
+              *reinterpret_cast<uint4*>(&join[row][e]) = make_uint4(y[e >> 5][e & 31], y[e >> 5][(e & 31) + 1], y[e >> 5][(e & 31) + 2], y[e >> 5][(e & 31) + 3]);
           rows_sync();
         }
         if (d0 == 0) {
@@ -721,11 +722,12 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
 #pragma unroll
           for (int e = 0; e < 64; e += 8) {
             const int d = d0 + e;
-            float x[8];
+            float x[8], other[8];
+            if constexpr (TWICE) Row<false>::get8(&join[row][e], other);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               x[i] = __uint_as_float(y[(e + i) >> 5][(e + i) & 31]);
-              if (TWICE) x[i] = x[i] * mine + join[row][e + i] * theirs;
+              if (TWICE) x[i] = x[i] * mine + other[i] * theirs;
               x[i] = fault ? __int_as_float(0x7fffffff) : x[i] * scale;
             }
             if (d < P.D) {
