@@ -5,6 +5,7 @@ given, no stream argument, tensors on the current device) go to the library nati
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import Optional, Sequence
 
@@ -134,6 +135,11 @@ class Rotation:
         return out
 
 
+def _allocating_on(stream: Optional[torch.cuda.Stream]):
+    """What a call allocates belongs to the stream that it runs on (memory of another stream's pool may still be in use there)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _check(rc: int, where: str) -> None:
     if rc != 0:
         raise LanternError(rc, where)
@@ -144,7 +150,8 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, rotation: Rotation, *, inve
     """lantern_rotary: rows x [B, R, H, D] turned by positions [axes, B, R].  inverse=True turns back, which is also the gradient with
     respect to x of a gradient with respect to the result.  out: a tensor like x, or x itself; allocated if not given."""
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        with _allocating_on(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if binding._call is not None and stream is None and rotation is not None:   # (loaded: the native part)
         rc = binding._call.rotary(x, positions, rotation._at, rotation._device, inverse, out)
         if rc is not None:
@@ -235,7 +242,8 @@ def cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, length
     if D != cache.head_dim or HQ % cache.heads:
         raise ValueError("q must have the cache's components and a multiple of its heads")
     if out is None:
-        out = (torch.empty if counts is None else torch.zeros)(q.shape, dtype=q.dtype, device=dev)
+        with _allocating_on(stream):
+            out = (torch.empty if counts is None else torch.zeros)(q.shape, dtype=q.dtype, device=dev)
     elif out.shape != q.shape or out.device != dev:
         raise ValueError("out must have q's shape")
     pt, width = _table(cache, table, B)
@@ -243,10 +251,7 @@ def cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, length
         if workspace is None:
             need = int(lib.lantern_cache_attention_workspace_bytes(dtype, B, R, HQ, cache._at, width))
             if need:
-                if stream is not None:
-                    with torch.cuda.stream(stream):
-                        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-                else:
+                with _allocating_on(stream):
                     workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         elif workspace.device != dev:
             raise ValueError(f"workspace must be on {dev}")
@@ -265,7 +270,8 @@ def cache_keep(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, accep
     """lantern_cache_keep: after verify(), moves the accepted path's tokens behind the root's and returns the sequences' new lengths (the
     root's and the path's tokens counted).  accept_len [B], accept_path [B, N] as verify() gives them."""
     if out_lengths is None:
-        out_lengths = torch.empty_like(lengths)
+        with _allocating_on(stream):
+            out_lengths = torch.empty_like(lengths)
     if binding._call is not None and stream is None:
         rc = binding._call.keep(cache._at, cache._device, table, lengths, accept_len, accept_path, out_lengths, status)
         if rc is not None:
@@ -302,7 +308,8 @@ def cache_read(cache: KVCache, table: torch.Tensor, first: torch.Tensor, rows: i
     dev = cache.device
     shape = (B, rows, cache.heads, cache.head_dim)
     if out is None:
-        out = tuple((torch.empty if counts is None else torch.zeros)(shape, dtype=dtype, device=dev) for _ in range(2))
+        with _allocating_on(stream):
+            out = tuple((torch.empty if counts is None else torch.zeros)(shape, dtype=dtype, device=dev) for _ in range(2))
     k, v = out
     if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != v.dtype or k.device != dev or v.device != dev:
         raise ValueError(f"out must be two tensors {list(shape)} on {dev}")

@@ -196,7 +196,8 @@ __device__ __forceinline__ float new_scale(float amax, float old, bool held, int
 
 // A CTA per touched block, run of heads and kind (keys or values): a block's angles are formed once for the heads of the run, then every head goes through
 // registers, U units of eight components per thread: maximum over the block, scale, codes.  Bound by the latency of a head's reads, the
-// maximum and the writes one after the other, and (keys) by the angles' arithmetic.
+// maximum and the writes one after the other, and (keys) by the angles' arithmetic (32 prompts of 0 to 1024 rows, 8 heads of 128: 53 us for 100 MB,
+// 34 without rotation; with angles formed in double precision and a read at a time 81; both kinds in one CTA 69).
 constexpr int AT = 256;
 template <bool BF16, int U>
 __global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) lantern_append_kernel(AppendParams P) {
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) 
 }
 
 // Few rows a sequence: a warp per touched block, head and kind.  The rows are read twice (the second time from L1); angles are formed by the
-// lane that needs them.  Bound by latency.
+// lane that needs them.  Bound by latency (128 sequences of one row, 8 heads: 6 us, most of it the launch).
 constexpr int FT = 128;
 template <bool BF16>
 __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) {
@@ -367,7 +368,8 @@ struct KeepParams {
 };
 
 // A warp per sequence, head and kind.  Targets ascend and no target lies behind its source (a path is increasing), so that going through the
-// targets in order, block by block, never overwrites a source that is still needed.  Bound by latency.
+// targets in order, block by block, never overwrites a source that is still needed.  Bound by latency: accepted path, table, scale, code one after the
+// other (256 trees, 20 heads: 11 us).
 constexpr int KT = 128;
 __global__ void __launch_bounds__(KT) lantern_keep_kernel(KeepParams P) {
   const int lane = threadIdx.x & 31;
@@ -465,7 +467,8 @@ struct ReadParams {
   int units;   // of a sequence: R * heads * D / 16
 };
 
-// A thread per 16 components of a row, keys and values.  Bound by HBM: one byte in, two or four out.
+// A thread per 16 components of a row, keys and values.  Bound by HBM: one byte in, two or four out (32 contexts of 4000 tokens, 8 heads of 128,
+// bf16: 146 us, 5.4 TB/s; 8 components a thread and two rows 154, 16 and two rows 158).
 constexpr int DT = 256;
 template <bool BF16>
 __global__ void __launch_bounds__(DT) lantern_read_kernel(ReadParams P) {

@@ -7,9 +7,10 @@
 // each and one tile ahead, and multiply 16 rows each by all of its tokens: m16n8k16 products of halves with fp32 accumulators, operands by
 // ldmatrix, scores and probabilities in registers.  Queries go in as halves after a power of two of their own (their 8 bits fit).
 //
-// Here the codes are few per product (two bytes for 2 x 64 of them), so that what costs is neither memory nor the tensor cores but what
-// lies between: many independent warps, each through its whole chain, hide that better than the one softmax warp per scheduler that a
-// CTA on the tcgen05 path has (cache_attention_wide.cu, which the same rows take in fp32 and more rows in either type).
+// What costs is neither memory nor the tensor cores alone: ldmatrix (every warp reads the whole tile) and the products keep shared memory and the
+// tensor pipe half busy each, and a warp's chain from scores to output does the rest.  256 trees of 61 rows, 20 heads of 64 components over 650
+// tokens: 360 us (1.4 TB/s of codes); codes turned into halves by every warp for itself 505; 32 rows a warp 472 (registers).
+// Where contexts can be long the tcgen05 path takes the same rows (cache_attention_wide.cu; both sides of the line are measured at `divide`).
 #include "cache_attention.cuh"
 
 namespace lantern {

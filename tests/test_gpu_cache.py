@@ -619,6 +619,27 @@ def test_two_streams_at_once():
     assert torch.equal(got, want[0]["o"])
 
 
+def test_results_belong_to_the_stream_of_the_call():
+    """What a call allocates comes from the pool of the stream it runs on: memory that the current stream has just given back, and still writes
+    to, is not the result's."""
+    cache, table, lengths, rows, pos, rot = small_step(150, R=20)
+    want = lt.rotary(rows[0], pos, rot), lt.cache_attention(rows[0], cache, table, lengths), lt.cache_read(cache, table, lengths, 7, counts=i32([7, 3, 0]))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        for t in (want[0], want[2][0]):
+            x = torch.empty_like(t)
+            torch.cuda._sleep(20_000_000)   # some ten milliseconds
+            x.fill_(3.0)
+            del x
+        got = (lt.rotary(rows[0], pos, rot, stream=side), lt.cache_attention(rows[0], cache, table, lengths, stream=side),
+               lt.cache_read(cache, table, lengths, 7, counts=i32([7, 3, 0]), stream=side))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1].view(torch.uint8), want[1].view(torch.uint8))
+        for a, b in zip(got[2], want[2]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 def test_a_cache_of_more_than_2_to_32_codes():
     H, S, D, pages = 8, 64, 128, 70_000   # 4.6e9 codes of each kind
     k = torch.empty((pages, H, S, D), dtype=torch.float8_e4m3fn, device="cuda")
