@@ -75,6 +75,37 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   const Unit u = unit_of(P, kRows, kTile, unit, static_cast<int>(blockIdx.x - unit * P.splits), unit_in(P, unit));
   grid_dependents_launch();
   if (!u.rows || u.split >= u.parts) return;
+  // ---- queries and the tree's parents: asked for before anything waits ----
+  const int g = lane >> 2, t = lane & 3;
+  int row_of[2];   // step row; -1: not there
+  uint32_t raw[2][KS][2];   // pairs of components 16 s + 2 t and 8 further
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int m = u.m0 + warp * 16 + g + 8 * half, r = m / P.G;
+    row_of[half] = r < u.n ? r : -1;
+    const T* p = static_cast<const T*>(P.q) + u.b * P.qs.b + r * P.qs.r + (static_cast<int64_t>(u.h) * P.G + (m - r * P.G)) * P.qs.h;
+    if (P.vec) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int d = 16 * s + 8 * k + 2 * t;
+          raw[half][s][k] = r < u.n && d < P.D ? __ldg(reinterpret_cast<const uint32_t*>(p + d)) : 0u;
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int d = 16 * s + 8 * k + 2 * t;
+          raw[half][s][k] = r < u.n && d < P.D ? static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(p + d))) |
+                                                     (static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(p + d + 1))) << 16)
+                                               : 0u;
+        }
+    }
+  }
+  const int32_t* parents = P.parents && !u.fault ? P.parents + static_cast<int64_t>(u.b) * (P.R - 1) : nullptr;
+  const int parent = parents && tid < u.n - 1 ? __ldg(parents + tid) : -1;
   const int words = (P.R + 31) >> 5, first_row = u.m0 / P.G, table_rows = (kRows + P.G - 1) / P.G + 1;
   if (tid == 0) {
     S.fault = u.fault;
@@ -115,34 +146,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   if (warp == 0)
     for (int i = 0; i < min(tiles, kStages); ++i) ask(i);
 
-  // ---- queries ----
-  const int g = lane >> 2, t = lane & 3;
+  // ---- queries: halves ----
   uint32_t q[KS][4];
   float factor[2];
-  int row_of[2];   // step row; -1: not there
   {
-    uint32_t raw[2][KS][2];   // pairs of components 16 s + 2 t and 8 further
-    const T* p[2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int m = u.m0 + warp * 16 + g + 8 * half, r = m / P.G;
-      row_of[half] = r < u.n ? r : -1;
-      p[half] = static_cast<const T*>(P.q) + u.b * P.qs.b + r * P.qs.r + (static_cast<int64_t>(u.h) * P.G + (m - r * P.G)) * P.qs.h;
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int d = 16 * s + 8 * k + 2 * t;
-          uint32_t w = 0;
-          if (row_of[half] >= 0 && d < P.D) {
-            if (P.vec) w = __ldg(reinterpret_cast<const uint32_t*>(p[half] + d));
-            else w = static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(p[half] + d))) | (static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(p[half] + d + 1))) << 16);
-          }
-          raw[half][s][k] = w;
-        }
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       float most = 0.0f;
@@ -175,11 +182,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
         }
     }
   }
-  if (P.parents && !u.fault) {
-    const int32_t* parents = P.parents + static_cast<int64_t>(u.b) * (P.R - 1);
+  if (parents) {
     int32_t* nodes = reinterpret_cast<int32_t*>(bits + table_rows * words);
     for (int i = tid; i < u.n - 1; i += 128) {
-      const int p = __ldg(parents + i);
+      const int p = i < 128 ? parent : __ldg(parents + i);
       nodes[i] = p;
       if (p < -1 || p >= i) atomicOr(&S.fault, LANTERN_ST_BAD_PARENT);
     }
