@@ -393,7 +393,7 @@ typedef struct {
 /* Rotates rows.  inverse != 0 turns by the negative angles, which is the rotation's transpose: the gradient with
  * respect to x is lantern_rotary(gradient of out, inverse = 1).
  *   x, out        [B, R, H, D], strides in elements (batch, row, head); out may be x itself (same strides), otherwise
- *                 they must not overlap
+ *                 they must not overlap; no two rows of out may be the same (a stride of 0: LANTERN_E_PARAM)
  *   B, R, H, D    B, R, H >= 0; 2 <= D <= 512, D even, 1 <= P <= D / 2, axes in [1, 4], every section >= 0 */
 lantern_status lantern_rotary(const void* x, void* out, int dtype, int B, int R, int H, int D, const int64_t x_stride[3],
                               const int64_t out_stride[3], const lantern_rotation* rotation, int inverse,
@@ -427,6 +427,9 @@ lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int
  * Scores, the softmax's maximum and sum and the outputs are fp32.  Queries enter the products as halves relative to the
  * row's largest component (bf16: exactly, but for components 2^28 times smaller than it; fp32: as two halves, 22 bits);
  * probabilities, relative to the row's largest, as halves (11 bits) with bf16 and as two halves with fp32.
+ * Values count relative to the largest value scale among the blocks that the rows taken together see: what is 2^-25 of 448
+ * times that scale or less may be lost for each token, so that blocks of very different scales are best kept in caches of
+ * their own.
  *
  *   q             [B, R, q_heads, D], strides in elements; 16-byte aligned rows are fastest, any alignment is served
  *   out           [B, R, q_heads, D] contiguous, dtype of q, 16-byte aligned; must not overlap q (out == q: LANTERN_E_PARAM)

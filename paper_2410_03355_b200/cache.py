@@ -77,7 +77,17 @@ def _index(t: Optional[torch.Tensor], shape, device, name: str):
     return _ptr(t, torch.int32, name)
 
 
-class KVCache:
+class _Fixed:
+    """An object whose tensors are those it was made of: the library is given their addresses, so that none may be put in another's place."""
+    __slots__ = ()
+
+    def __setattr__(self, name, value):
+        if hasattr(self, "_device"):   # (set last)
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+
+class KVCache(_Fixed):
     """A paged cache of one layer's keys and values in 8 bits: codes k, v [pages, heads, page_tokens, head_dim] float8_e4m3fn, and a
     scale for each page and head, k_scale, v_scale [pages, heads] float32 (see lantern_cache in include/lantern.h)."""
     __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "heads", "page_tokens", "head_dim", "device", "_struct", "_at", "_device")
@@ -107,7 +117,7 @@ class KVCache:
         return cls(*code, *(torch.ones((pages, heads), dtype=torch.float32, device=device) for _ in range(2)))
 
 
-class Rotation:
+class Rotation(_Fixed):
     """Rotary frequencies: inv_freq [P] float32, the number of pairs of each axis, and which components make a pair -- (2j, 2j+1) if
     interleaved, else (j, j+P) (see lantern_rotation in include/lantern.h)."""
     __slots__ = ("inv_freq", "sections", "interleaved", "_struct", "_at", "_device")

@@ -691,6 +691,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (m - r * P.G)) * P.D;
       float* to = P.parts + part * DP;
       float scale = 0.0f;
+      // What the last unit's rows still read: with tiles the wait for values_free says that they are done (it takes every warp's probabilities).
+      if (TWICE && tiles == 0) rows_sync();
       if (TWICE && group == 1) S.ml[row] = make_float2(ref, sum);
 #pragma unroll
       for (int d0 = 0; d0 < DP; d0 += 64) {   // (a thread that waits for products of the next unit is not ahead of one that still reads here)
@@ -745,7 +747,6 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         }
       }
       if (group == 0 && there && !whole) P.part_ml[part] = make_float2(ref, fault ? __int_as_float(0x7fffffff) : L);
-      if (TWICE && tiles == 0) rows_sync();   // (nothing else would keep the next unit from writing what is read here)
       if (tiles > 0) ++slot;
     }
   }

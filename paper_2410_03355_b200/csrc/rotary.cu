@@ -132,6 +132,7 @@ extern "C" lantern_status lantern_rotary(const void* x, void* out, int dtype, in
   if (P.rows > INT32_MAX || static_cast<int64_t>(H) * D > INT32_MAX / 2) return LANTERN_E_SHAPE;
   if (P.rows == 0 || H == 0) return LANTERN_OK;
   if (!x || !out) return LANTERN_E_NULL;
+  if ((B > 1 && out_stride[0] == 0) || (R > 1 && out_stride[1] == 0) || (H > 1 && out_stride[2] == 0)) return LANTERN_E_PARAM;   // (one row for several)
   P.x = x;
   P.out = out;
   P.xs = {x_stride[0], x_stride[1], x_stride[2]};

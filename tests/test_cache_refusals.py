@@ -126,6 +126,14 @@ def test_rotary():
     assert rotary(out=AT + 1) == ALIGN
 
 
+def test_rotary_rows_that_are_one():
+    for axis in range(3):
+        stride = [4 * 64 * 3, 4 * 64, 64]
+        stride[axis] = 0
+        call = lambda shape: lt.load_library().lantern_rotary(AT, 2 * AT, lt.BF16, *shape, strides(), (ctypes.c_int64 * 3)(*stride), ref(rotation()), 0, None)
+        assert call((2, 3, 4, 64)) == PARAM
+
+
 def test_binding_refuses_what_it_cannot_marshal():
     f8 = torch.zeros(4, 2, 16, 16, dtype=torch.uint8).view(torch.float8_e4m3fn)
     with pytest.raises(ValueError, match="CUDA"):

@@ -461,6 +461,56 @@ def test_attention_more_units_than_places(D, R, tree, dtype):
     run_attention(lengths, R, 7, 1, D, 16, dtype, tree=tree, counts=counts, starts=starts)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_blank_units_between_others(D, dtype):
+    """Sequences whose rows see nothing, or that are refused, take turns with others on the same CTAs: they change nothing of these."""
+    S, R, width, each = 16, 17, 144, 296     # (a multiple of the places for CTAs)
+    B = 6 * each
+    pages = 40
+    table = make_table(pages // 4, 4, pages, 63)
+    cache = filled_cache(table, [60] * (pages // 4), 1, S, D, pages, 64)
+    g = gen(65)
+    wide = torch.zeros(B, width, dtype=torch.int32, device="cuda")
+    wide[:, :4] = table[torch.arange(B) % (pages // 4)].to("cuda")
+    lengths = torch.randint(1, 40, (B,), generator=g)
+    turn = (torch.arange(B) // each) % 6
+    starts = torch.where(turn % 3 == 1, 100, 0)
+    blank, refused = turn % 3 == 1, turn == 5
+    lengths[refused] = -1
+    q = normal((B, R, 1, D), 66, dtype)
+    some = ~(blank | refused)
+    want = lt.cache_attention(q[some.cuda()].contiguous(), cache, wide[some.cuda()].contiguous(), i32(lengths[some].tolist()))
+    for _ in range(5):
+        status = torch.zeros(B, dtype=torch.int32, device="cuda")
+        got = lt.cache_attention(q, cache, wide, i32(lengths.tolist()), starts=i32(starts.tolist()), status=status)
+        assert torch.equal(got[some.cuda()], want)
+        assert not got[blank.cuda()].any() and got[refused.cuda()].isnan().all()
+        assert status.tolist() == [lt.ST_BAD_LENGTH if r else 0 for r in refused.tolist()]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("R,H,D", [(1, 2, 64), (30, 2, 128), (40, 1, 64), (90, 1, 96)])
+def test_attention_value_scales_far_apart(R, H, D, dtype):
+    S, lengths = 16, [150, 97]
+    width = -(-(max(lengths) + R) // S)
+    table = make_table(2, width, 2 * width, 67)
+    cache = filled_cache(table, [n + R for n in lengths], H, S, D, 2 * width, 68)
+    cache.v_scale.copy_(torch.exp2(torch.randint(-60, 30, cache.v_scale.shape, generator=gen(69)).float()))
+    q = normal((2, R, H, D), 70, dtype)
+    got = lt.cache_attention(q, cache, table, i32(lengths))
+    want, bound = ref.attention(q.cpu(), snapshot(cache), table.tolist(), lengths)
+    close(got, want, bound, dtype)
+
+
+def test_caches_and_rotations_are_fixed():
+    cache = lt.KVCache.empty(2, 1, 16, 16)
+    rotation = lt.Rotation(torch.ones(4, device="cuda"), (4,), interleaved=True)
+    for made, name in ((cache, "k"), (cache, "v_scale"), (cache, "heads"), (rotation, "inv_freq"), (rotation, "interleaved")):
+        with pytest.raises(AttributeError, match="fixed"):
+            setattr(made, name, getattr(made, name))
+
+
 def test_attention_largest_tree():
     run_attention([70], 1025, 1, 1, 16, 64, BF, tree=100)
 
