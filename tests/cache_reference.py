@@ -140,8 +140,10 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
                     # Scores: D products summed in fp32, whose every addition may drop up to a unit of the last place (2^-23) of the
                     # running sum of magnitudes; queries to 2^-17 (of the largest, as halves with a common exponent: far less) or, in
                     # fp32, 2^-22; three roundings more and those of the base-2 argument.  Numerators: exp2 2^-22, the sum of n of them
-                    # 2^-24 each; as a half 2^-11 (as two 2^-22) and, below the smallest normal half, 2^-25 of the largest value.
+                    # 2^-24 each; as a half 2^-11 (as two 2^-22) and, below the smallest normal half 2^-14, 2^-25 of the largest value:
+                    # halves there are 2^-24 apart.  What the first of two halves leaves of a numerator p < 1 is at most 2^-12, mostly below
+                    # 2^-14 and so rounded by up to 2^-25 in the second, too: the term is the same for both types.
                     score = size.max().item() * ((D + 8) * 2.0 ** -23 + 2.0 ** -21)
                     rel = 2.0 * score + 2.0 ** -21 + len(see) * 2.0 ** -23 + (2.0 ** -21 if f32 else 2.0 ** -11)
-                    bound[b, r, g] = rel * (p @ v[see, h].abs()) + rel * out[b, r, g].abs() + len(see) * 2.0 ** (-35 if f32 else -25) * vmax
+                    bound[b, r, g] = rel * (p @ v[see, h].abs()) + rel * out[b, r, g].abs() + len(see) * 2.0 ** -25 * vmax
     return out, bound
