@@ -91,24 +91,39 @@ __device__ __forceinline__ void widen8(const Raw<BF16>& r, float (&v)[8]) {
       v[4 * i] = __uint_as_float(r.w[i].x), v[4 * i + 1] = __uint_as_float(r.w[i].y), v[4 * i + 2] = __uint_as_float(r.w[i].z), v[4 * i + 3] = __uint_as_float(r.w[i].w);
   }
 }
+// A row of the table of cosines and sines has its pairs two by two (16 bytes), exchanged among eights so that neighbours, which read eight pairs (or
+// four) each, find different banks.  Rows are padded to eights.
+__device__ __forceinline__ int eights(int pairs) { return (pairs + 7) & ~7; }
+__device__ __forceinline__ int place_of(int pair) { return pair ^ (((pair >> 4) & 3) << 1); }
+__device__ __forceinline__ float4 two_angles(const float2* table, int pair) { return *reinterpret_cast<const float4*>(table + place_of(pair)); }   // pair even
 // Eight keys turned: v their components from d on, o their partners' in the other half (if not interleaved).
 __device__ __forceinline__ void turn8(const Rotation& rot, int d, const float2* table, float (&v)[8], const float (&o)[8]) {
   const int pairs = rot.pairs;
+  if (d >= 2 * pairs) return;
   if (rot.interleaved) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      if (d + i < 2 * pairs) {
-        const float2 w = table[(d + i) >> 1];
-        const float a = v[i], b = v[i + 1];
-        v[i] = turned_low(a, b, w);
-        v[i + 1] = turned_high(a, b, w);
+    for (int i = 0; i < 8; i += 4) {
+      const float4 ww = two_angles(table, (d + i) >> 1);
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        if (d + i + e < 2 * pairs) {
+          const float2 w = e ? make_float2(ww.z, ww.w) : make_float2(ww.x, ww.y);
+          const float a = v[i + e], b = v[i + e + 1];
+          v[i + e] = turned_low(a, b, w);
+          v[i + e + 1] = turned_high(a, b, w);
+        }
       }
     }
-  } else if (d < 2 * pairs) {
+  } else {
     const bool lower = d < pairs;
-    const float2* w = table + (lower ? d : d - pairs);
+    const int j = lower ? d : d - pairs;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = lower ? turned_low(v[i], o[i], w[i]) : turned_high(o[i], v[i], w[i]);
+    for (int i = 0; i < 8; i += 2) {
+      const float4 ww = two_angles(table, j + i);
+      const float2 w0 = make_float2(ww.x, ww.y), w1 = make_float2(ww.z, ww.w);
+      v[i] = lower ? turned_low(v[i], o[i], w0) : turned_high(o[i], v[i], w0);
+      v[i + 1] = lower ? turned_low(v[i + 1], o[i + 1], w1) : turned_high(o[i + 1], v[i + 1], w1);
+    }
   }
 }
 
@@ -128,7 +143,7 @@ __device__ __forceinline__ void new_values(const AppendParams& P, const typename
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       if (d + i < 2 * pairs) {
-        const float2 w = table[(d + i) >> 1];
+        const float2 w = table[place_of((d + i) >> 1)];
         const float a = v[i], b = v[i + 1];
         v[i] = turned_low(a, b, w);
         v[i + 1] = turned_high(a, b, w);
@@ -141,7 +156,7 @@ __device__ __forceinline__ void new_values(const AppendParams& P, const typename
     Row<BF16>::get8(p + (lower ? d + pairs : d - pairs), o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float2 w = table[j + i];
+      const float2 w = table[place_of(j + i)];
       v[i] = lower ? turned_low(v[i], o[i], w) : turned_high(o[i], v[i], w);
     }
   } else {
@@ -150,7 +165,7 @@ __device__ __forceinline__ void new_values(const AppendParams& P, const typename
       if (d + i < 2 * pairs) {
         const bool lower = d + i < pairs;
         const int j = lower ? d + i : d + i - pairs;
-        const float2 w = table[j];
+        const float2 w = table[place_of(j)];
         const float o = Row<BF16>::get(p + (lower ? d + i + pairs : j));
         v[i] = lower ? turned_low(v[i], o, w) : turned_high(o, v[i], w);
       }
@@ -196,13 +211,13 @@ __device__ __forceinline__ float new_scale(float amax, float old, bool held, int
 
 // A CTA per touched block, run of heads and kind (keys or values): a block's angles are formed once for the heads of the run, then every head goes through
 // registers, U units of eight components per thread: maximum over the block, scale, codes.  Bound by the latency of a head's reads, the
-// maximum and the writes one after the other, and (keys) by the angles' arithmetic (32 prompts of 0 to 1024 rows, 8 heads of 128: 53 us for 100 MB,
-// 34 without rotation; with angles formed in double precision and a read at a time 81; both kinds in one CTA 69).
-constexpr int AT = 256;
-template <bool BF16, int U>
-__global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) lantern_append_kernel(AppendParams P) {
+// maximum and the writes one after the other, and (keys) by the angles' arithmetic (32 prompts of 0 to 1024 rows, 8 heads of 128: 47 us for 100 MB,
+// 33 without rotation; 53 with the angles in their order, eight threads to a bank; with angles formed in double precision and a read at a time 81;
+// both kinds in one CTA 69; the next head's reads under way ahead of this one's maximum: fp32 blocks of 32 tokens 74 -> 82 with the read, for registers).
+template <bool BF16, int AT, int U>   // AT threads
+__global__ void __launch_bounds__(AT, (U == 1 ? 5 : U == 2 ? 4 : 2) * 256 / AT) lantern_append_kernel(AppendParams P) {
   using T = typename Row<BF16>::T;
-  extern __shared__ float2 angles[];   // [new slots][pairs]
+  extern __shared__ __align__(16) float2 angles[];   // [new slots][eights of pairs]
   __shared__ float most[2][AT / 32];
   __shared__ uint64_t steps[kMaxHeadDim / 2];
   const int b = blockIdx.z, j = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -220,7 +235,7 @@ __global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) 
     const uint64_t step = steps[k];
     if (t0 < at_once)
 #pragma unroll 2
-      for (int t = t0; t < n; t += at_once) angles[t * pairs + k] = turn_by(step, position_of(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, k));
+      for (int t = t0; t < n; t += at_once) angles[t * eights(pairs) + place_of(k)] = turn_by(step, position_of(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, k));
   }
   // A thread keeps its eight components d.. of a row and goes through rows t0, t0 + at_once, ...
   const int D = P.c.D, per_row = D >> 3, at_once = AT / per_row, t0 = tid / per_row, d = (tid - t0 * per_row) * 8;
@@ -251,7 +266,7 @@ __global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) 
             if (turns) {
               float o[8];
               if (partners) widen8<BF16>(other[u], o);
-              turn8(P.rot, d, angles + t * pairs, v[u], o);
+              turn8(P.rot, d, angles + t * eights(pairs), v[u], o);
             }
             m = fmaxf(m, magnitude(v[u], odd));
           }
@@ -262,7 +277,7 @@ __global__ void __launch_bounds__(AT, U == 1 ? 5 : U == 2 ? 4 : U == 4 ? 2 : 1) 
         for (int u = 0; u < U; ++u) {
           const int t = t0 + u * at_once;
           if (works && t < n) {
-            new_values<BF16>(P, x + (s.row + t) * P.xs[which].r, d, turns ? angles + t * pairs : nullptr, v[u]);
+            new_values<BF16>(P, x + (s.row + t) * P.xs[which].r, d, turns ? angles + t * eights(pairs) : nullptr, v[u]);
             m = fmaxf(m, magnitude(v[u], odd));
           }
         }
@@ -301,7 +316,7 @@ constexpr int FT = 128;
 template <bool BF16>
 __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) {
   using T = typename Row<BF16>::T;
-  __shared__ float2 angles[FT / 32][kMaxHeadDim / 2];
+  __shared__ __align__(16) float2 angles[FT / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int item = blockIdx.x * (FT / 32) + warp;   // (head, kind)
   const int b = blockIdx.z, j = blockIdx.y;
@@ -322,7 +337,7 @@ __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) 
     const T* p = x + (s.row + t) * P.xs[which].r;
     if (rotate) {
       __syncwarp();
-      for (int i = lane; i < P.rot.pairs; i += 32) angles[warp][i] = turn(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, i);
+      for (int i = lane; i < P.rot.pairs; i += 32) angles[warp][place_of(i)] = turn(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, i);
       __syncwarp();
     }
     if (lane < per_row) new_values<BF16>(P, p, lane * 8, rotate ? angles[warp] : nullptr, v);
@@ -346,12 +361,12 @@ __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) 
   if (odd && P.status) atomicOr(P.status + b, LANTERN_ST_NONFINITE);
 }
 
-template <bool BF16, int U>
+template <bool BF16, int AT, int U>
 static cudaError_t launch_append(const AppendParams& P, dim3 grid, size_t smem, cudaStream_t st) {
   static DeviceFlags ready;
-  const cudaError_t e = allow_shared_memory(lantern_append_kernel<BF16, U>, 128 * (kMaxHeadDim / 2) * sizeof(float2), ready);
+  const cudaError_t e = allow_shared_memory(lantern_append_kernel<BF16, AT, U>, 128 * (kMaxHeadDim / 2) * sizeof(float2), ready);
   if (e != cudaSuccess) return e;
-  lantern_append_kernel<BF16, U><<<grid, AT, smem, st>>>(P);
+  lantern_append_kernel<BF16, AT, U><<<grid, AT, smem, st>>>(P);
   return cudaGetLastError();
 }
 
@@ -563,12 +578,14 @@ extern "C" lantern_status lantern_cache_append(const void* k, const void* v, int
     const int64_t per = static_cast<int64_t>(B) * touched * 2 * H / (8 * 148), most = H < 4 ? H : 4;
     P.heads_per_cta = static_cast<int>(per < 1 ? 1 : per > most ? most : per);
     const dim3 grid(2 * ((H + P.heads_per_cta - 1) / P.heads_per_cta), static_cast<unsigned>(touched), B);
-    const size_t smem = rotation ? static_cast<size_t>(S) * P.rot.pairs * sizeof(float2) : 0;
-    const int at_once = AT / (D / 8), u = (S + at_once - 1) / at_once;   // rows at a time; at most 8 times
-    if (u <= 1) e = bf ? launch_append<true, 1>(P, grid, smem, st) : launch_append<false, 1>(P, grid, smem, st);
-    else if (u <= 2) e = bf ? launch_append<true, 2>(P, grid, smem, st) : launch_append<false, 2>(P, grid, smem, st);
-    else if (u <= 4) e = bf ? launch_append<true, 4>(P, grid, smem, st) : launch_append<false, 4>(P, grid, smem, st);
-    else e = bf ? launch_append<true, 8>(P, grid, smem, st) : launch_append<false, 8>(P, grid, smem, st);
+    const size_t smem = rotation ? static_cast<size_t>(S) * ((P.rot.pairs + 7) & ~7) * sizeof(float2) : 0;
+    // Units of eight components for each of 256 threads: at most 8.  Where they take so many registers that a CTA leaves no room for others, 512 threads
+    // (with the read, fp32 blocks of 64 tokens of 128: 85 -> 82 us, bf16 ones of 128: 103 -> 91; bf16 of 64: 75 and 76).
+    const int u = (S + 256 / (D / 8) - 1) / (256 / (D / 8));
+    if (u <= 1) e = bf ? launch_append<true, 256, 1>(P, grid, smem, st) : launch_append<false, 256, 1>(P, grid, smem, st);
+    else if (u <= 2) e = bf ? launch_append<true, 256, 2>(P, grid, smem, st) : launch_append<false, 256, 2>(P, grid, smem, st);
+    else if (u <= 4) e = bf ? launch_append<true, 256, 4>(P, grid, smem, st) : launch_append<false, 512, 2>(P, grid, smem, st);
+    else e = bf ? launch_append<true, 512, 4>(P, grid, smem, st) : launch_append<false, 512, 4>(P, grid, smem, st);
   }
   return e == cudaSuccess ? LANTERN_OK : LANTERN_E_CUDA;
 }
