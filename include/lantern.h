@@ -426,10 +426,11 @@ lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int
  *
  * Scores, the softmax's maximum and sum and the outputs are fp32.  Queries enter the products as halves relative to the
  * row's largest component (bf16: exactly, but for components 2^28 times smaller than it; fp32: as two halves, 22 bits);
- * probabilities, relative to the row's largest, as halves (11 bits) with bf16 and as two halves with fp32.
- * Values count relative to the largest value scale among the blocks that the rows taken together see: what is 2^-25 of 448
- * times that scale or less may be lost for each token, so that blocks of very different scales are best kept in caches of
- * their own.
+ * probabilities as halves (11 bits) with bf16 and as two halves (22 bits) with fp32, but with an end to their bits: for
+ * EACH token up to 2^-35 of the row's largest probability, times its code under the largest value scale among the blocks that
+ * the rows taken together see, is lost from the numerator (not from the sum).  n tokens that far behind one that has next to
+ * no value of its own can so lose n * 2^-35 of that one's weight between them: 3e-6 for 100 000 tokens.  What of a value is
+ * below 2^-32 of the largest value scale may be lost as well.
  *
  *   q             [B, R, q_heads, D], strides in elements; 16-byte aligned rows are fastest, any alignment is served
  *   out           [B, R, q_heads, D] contiguous, dtype of q, 16-byte aligned; must not overlap q (out == q: LANTERN_E_PARAM)

@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
     }
     float f[NQ][2][2];   // of a row and 16 tokens
     const float v_most = fmaxf(vs[0], vs[1]);
-    bool grow = v_most > vref * 32.0f;
+    bool grow = v_most > vref * kScaleLag;
     float most[NQ][2];
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
@@ -268,10 +268,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
         m = fmaxf(m, __shfl_xor_sync(kFull, m, 8));
         m = fmaxf(m, __shfl_xor_sync(kFull, m, 16));
         most[q][e] = m;
-        grow |= m > ref[q][e] + 8.0f;
+        grow |= m > ref[q][e] + kLag;
       }
-    // The maximum that the numerators refer to follows the running maximum only when it has fallen behind by 2^8 (the reference scale of the
-    // values: 2^5), so that the accumulators are rarely touched; a numerator stays below 2^8 * 2^5, a half's largest value is 2^16.
     if (__any_sync(kFull, grow)) {
       const float v_new = fmaxf(vref, v_most), v_ratio = v_new > 0.0f ? vref / v_new : 0.0f;
 #pragma unroll
@@ -292,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {   // 16 tokens
-      const float vr = vs[k] * v_over;
+      const float vr = vs[k] * v_over * kLift;
       uint32_t p[NQ][TERMS][2];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
@@ -367,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
       float M = -INFINITY;
 #pragma unroll
       for (int k = 0; k < kWarps; ++k) M = fmaxf(M, S.ml[k][row].x);
-      const float w = vref * ex2_approx(ref[q][e] - (M == -INFINITY ? 0.0f : M));
+      const float w = vref * (1.0f / kLift) * ex2_approx(ref[q][e] - (M == -INFINITY ? 0.0f : M));
 #pragma unroll
       for (int n = 0; n < MT; n += 2)
         *reinterpret_cast<float4*>(buf + (warp * 8 * NQ + row) * (DP + 4) + VL * g + 2 * n) =

@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
     float f[2][SG], most[2], v_most = vs[0];
 #pragma unroll
     for (int k = 1; k < SG; ++k) v_most = fmaxf(v_most, vs[k]);
-    bool grow = v_most > vref * 32.0f;
+    bool grow = v_most > vref * kScaleLag;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       float m = -INFINITY;
@@ -327,11 +327,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
         m = fmaxf(m, a * f[half][k]);
       }
       most[half] = m;   // of this lane's tokens
-      grow |= m > ref[half] + 8.0f;
+      grow |= m > ref[half] + kLag;
     }
-    // The maximum that the numerators refer to follows the running maximum only when it has fallen behind by 2^8 (the reference scale of the
-    // values: 2^5), so that the accumulators are rarely touched -- and the lanes' maxima rarely put together; a numerator stays below 2^8 * 2^5, a
-    // half's largest value is 2^16.
+    // (the lanes' maxima are put together only when the reference moves)
     if (__any_sync(kFull, grow)) {
       const float v_new = fmaxf(vref, v_most), v_ratio = v_new > 0.0f ? vref / v_new : 0.0f;
       float w[2];
@@ -354,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
 #pragma unroll
     for (int k = 0; k < SG; ++k) {   // 16 tokens
       uint32_t p[4];
-      const __half2 vr = __float2half2_rn(vs[k] * v_over);
+      const float vr = vs[k] * v_over * kLift;
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -363,9 +361,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
           unpack2(fma2(pack2(c[2 * k + j][2 * half], c[2 * k + j][2 * half + 1]), pack2(f[half][k], f[half][k]), pack2(back[half], back[half])), a, b);
           a = ex2_approx(a), b = ex2_approx(b);
           part[half] = add2(part[half], pack2(a, b));
-          uint32_t h = half2_of(a, b);
-          const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h), vr);
-          p[2 * j + half] = *reinterpret_cast<const uint32_t*>(&y);
+          unpack2(mul2(pack2(a, b), pack2(vr, vr)), a, b);
+          p[2 * j + half] = half2_of(a, b);
         }
 #pragma unroll
       for (int n = 0; n < NT; n += 2) {
@@ -413,7 +410,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
     const int m = u.m0 + row;
     T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (m - r * P.G)) * P.D;
     float* to = P.parts + (part + row) * DP;
-    const float scale = fault ? __int_as_float(0x7fffffff) : whole ? (sum[half] == 0.0f ? 0.0f : vref / sum[half]) : vref;
+    const float own = vref * (1.0f / kLift);
+    const float scale = fault ? __int_as_float(0x7fffffff) : whole ? (sum[half] == 0.0f ? 0.0f : own / sum[half]) : own;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int d = 8 * n + 2 * t;

@@ -5,7 +5,7 @@
 // A CTA takes 128 rows of one sequence and cache head and a part of the tokens:
 //   - a producer warp copies a tile of codes per stage (TMA, block by block through the table);
 //   - four warps turn codes into halves (every e4m3 value is one) in the layout that the products read, values times their scale over the part's
-//     largest (a power of two: exact);
+//     largest (a power of two: exact) and times 2^7, which is the room that a half leaves above 448;
 //   - one thread issues scores = queries . keys and output += probabilities . values, 128 rows wide, queries and probabilities out of tensor
 //     memory, one tile of scores ahead of the softmax;
 //   - four warps, a thread per row, take the scores from tensor memory, keep the row's running maximum and sum and put the probabilities
@@ -39,6 +39,7 @@ struct Shape {
 
 enum { kFirst = 1, kLast = 2, kEnd = 4, kEdge = 8 };   // of a tile: of its unit; there are no more; some row may not see all of its tokens
 
+constexpr float kValueLift = 128.0f;
 constexpr int kJoinRow = 68;   // (rows 16 bytes apart in the banks)
 constexpr int kSlots = 8;   // units that can be under way: one per tile in the stages, in the halves and in the scores, at most
 template <int DP>
@@ -46,7 +47,7 @@ struct WideShared {
   static constexpr int kTile = Shape<DP>::kTile, kStages = Shape<DP>::kStages;
   uint64_t full[kStages], empty[kStages];
   uint64_t keys_full[2], keys_free[2], values_full[2], values_free[2], scores_full[2], probs_full[2], query_full;
-  float scale[kStages][2][kTile / 16];   // of every 16 tokens: keys; values, over the largest of the part
+  float scale[kStages][2][kTile / 16];   // of every 16 tokens: keys; values, over the largest of the part, lifted
   int flags[kStages];                    // of a stage's tile
   float key_scale[4][kTile / 16];        // of the tiles whose scores are under way
   int tile_flags[4];
@@ -146,6 +147,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
   using C = Shape<DP>;
   constexpr int TILE = C::kTile, STAGES = C::kStages;
   constexpr int TERMS = BF16 ? 1 : 2, ROWS = TWICE ? 64 : 128;
+  // Numerators are lifted with the argument of exp2, the sum with them (bf16: the argument's rounding is then 2^-21), or by a product (fp32).
+  constexpr float kRaise = BF16 ? 10.0f : 0.0f, kSumLift = BF16 ? kLift : 1.0f;
+  static_assert(kLift == 1024.0f, "2^10");
   constexpr int RUN = TILE * 128;   // bytes of 64 components of a tile of halves
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* halves = smem + STAGES * C::kRaw;   // [2][keys, values]
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         if (turn)
           for (int e = 0; e < sub / 16; ++e) {
             S.scale[stage][0][my_sub / 16 + e] = x.ks;
-            S.scale[stage][1][my_sub / 16 + e] = most > 0.0f ? x.vs / most : 0.0f;
+            S.scale[stage][1][my_sub / 16 + e] = most > 0.0f ? x.vs / most * kValueLift : 0.0f;
           }
         const int token0 = (u.tile0 + u.lo + i) * TILE;
         const int any_fault = __reduce_or_sync(kFull, fault);
@@ -612,9 +616,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
           factors(j, fa, fb);
           top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]) * fa, fmaxf(a[2], a[3]) * fb));
         }
-        // The maximum that the probabilities refer to follows the running maximum only when it has fallen behind by 2^8 (a half holds 2^16), so
-        // that the accumulators are rarely touched.
-        if (__any_sync(kFull, top > ref + 8.0f)) {
+        if (__any_sync(kFull, top > ref + kLag)) {   // (the probabilities' reference)
           const float to = fmaxf(ref, top), w = ref == -INFINITY ? 0.0f : ex2_approx(ref - to);
           ref = to;
           sum *= w;
@@ -632,7 +634,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
             }
           }
         }
-        const float base = ref == -INFINITY ? 0.0f : ref;
+        const float base = ref == -INFINITY ? 0.0f : ref - kRaise;
         uint64_t part[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
         const uint64_t back = pack2(-base, -base);
 #pragma unroll UNROLL
@@ -649,6 +651,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
             unpack2(fma2(pack2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), pack2(ff, ff), back), a, b);
             a = ex2_approx(a), b = ex2_approx(b);
             part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pack2(a, b));
+            if constexpr (!BF16) unpack2(mul2(pack2(a, b), pack2(kLift, kLift)), a, b);
             h[e / 2] = half2_of(a, b);
             if constexpr (TERMS == 2) l[e / 2] = half2_rest(a, b, h[e / 2]);
           }
@@ -683,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       }
       if (!ok) fault |= LANTERN_ST_INTERNAL;
       if (fault && tid == 0 && P.status) atomicOr(P.status + u.b, fault);
-      const float vref = tiles > 0 ? S.vref[slot & (kSlots - 1)] : 0.0f;
+      const float vref = tiles > 0 ? S.vref[slot & (kSlots - 1)] * (1.0f / (kLift * kValueLift)) : 0.0f;
       const bool whole = u.parts == 1;
       float mine = 1.0f, theirs = 0.0f;   // weights of this half's accumulators and of the other's
       float L = sum;
@@ -721,6 +724,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
             L = sum * mine + other.y * theirs;
             ref = M;
           }
+          L *= 1.0f / kSumLift;
           scale = whole ? (L == 0.0f ? 0.0f : vref / L) : vref;
         }
         if (group == 0 && there) {
