@@ -5,7 +5,8 @@
 // A CTA takes 128 rows of one sequence and cache head and a part of the tokens:
 //   - a producer warp copies a tile of codes per stage (TMA, block by block through the table);
 //   - four warps turn codes into halves (every e4m3 value is one) in the layout that the products read, values times their scale over the part's
-//     largest (a power of two: exact) and times 2^7, which is the room that a half leaves above 448;
+//     largest and times 2^7, which is the room that a half leaves above 448 -- exact where scales are powers of two, as append leaves them; where a caller's are
+//     not, rounded to a half's 11 bits with bf16, while with fp32 only the power of two goes with the value and the scale's digits go with the probabilities;
 //   - one thread issues scores = queries . keys and output += probabilities . values, 128 rows wide, queries and probabilities out of tensor
 //     memory, one tile of scores ahead of the softmax;
 //   - four warps, a thread per row, take the scores from tensor memory, keep the row's running maximum and sum and put the probabilities
@@ -50,6 +51,7 @@ struct WideShared {
   float scale[kStages][2][kTile / 16];   // of every 16 tokens: keys; values, over the largest of the part, lifted
   int flags[kStages];                    // of a stage's tile
   float key_scale[4][kTile / 16];        // of the tiles whose scores are under way
+  float lift[4][kTile / 16];             // fp32: kLift times the digits (1 to 2) of the value scale
   int tile_flags[4];
   uint32_t bad[4][4];                    // tokens with a NaN among their values, by converting warp
   float vref[kSlots];
@@ -128,6 +130,12 @@ __device__ __forceinline__ uint32_t times(uint32_t halves, __half2 ratio) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&halves), ratio);
   return *reinterpret_cast<const uint32_t*>(&r);
 }
+// x is a power of two (zero, or what is not finite, as it is) times its digits, 1 to 2
+__device__ __forceinline__ float power_of(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return (b & 0x7f800000u) == 0x7f800000u ? x : __uint_as_float(b & 0xff800000u);
+}
+__device__ __forceinline__ float digits_of(float x) { return __uint_as_float((__float_as_uint(x) & 0x7fffffu) | 0x3f800000u); }
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 __device__ __forceinline__ void rows_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }   // of the softmax warps
@@ -237,6 +245,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         if (x.mine) most = fmaxf(most, x.vs);
       }
       most = warp_max(most);
+      if (!BF16) most = fmaxf(power_of(most), 1.17549435e-38f);   // (so that quotients are exact)
       if (lane == 0) S.vref[slot & (kSlots - 1)] = most;
       const int first_row = u.m0 / P.G;
       int fault = late;
@@ -360,7 +369,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       const bool edge = flags & kEdge;
       const uint8_t* raw = smem + stage * C::kRaw;
       if (share == 0 && (token & 15) == 0) S.key_scale[at][token >> 4] = S.scale[stage][0][token >> 4];
-      const __half2 ratio = __float2half2_rn(S.scale[stage][1][token >> 4]);
+      const float factor = S.scale[stage][1][token >> 4];
+      const __half2 ratio = __float2half2_rn(BF16 ? factor : power_of(factor));
+      if (!BF16 && share == 0 && (token & 15) == 0) S.lift[at][token >> 4] = kLift * digits_of(factor);
       bool nan = false;
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
@@ -651,7 +662,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
             unpack2(fma2(pack2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), pack2(ff, ff), back), a, b);
             a = ex2_approx(a), b = ex2_approx(b);
             part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pack2(a, b));
-            if constexpr (!BF16) unpack2(mul2(pack2(a, b), pack2(kLift, kLift)), a, b);
+            if constexpr (!BF16) {
+              const float up = S.lift[n & 3][2 * (c0 + j) + (e < 16 ? 0 : 1)];
+              unpack2(mul2(pack2(a, b), pack2(up, up)), a, b);
+            }
             h[e / 2] = half2_of(a, b);
             if constexpr (TERMS == 2) l[e / 2] = half2_rest(a, b, h[e / 2]);
           }

@@ -37,7 +37,8 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
     * Numerators.  exp2 to 2^-22; rounded once as a half, 2^-11 (bf16), or as two, 2^-22 (fp32), after a product with the value's scale (2^-23).  They are
       lifted by 2^10, so that what lies below the smallest normal half loses 2^-25 * 2^-10 of the row's largest numerator, as a factor of a code under the largest
       value scale that the row's blocks have.
-    * Values become halves times 2^7 over the largest scale: off by 2^-25 * 2^-7 of it (2 where a scale's own digits are put with the numerators).
+    * Values become halves times 2^7 over the largest scale: off by 2^-25 * 2^-7 of it (2 where a scale's own digits are put with the numerators), and with bf16,
+      where a scale is no power of two, by 2^-11 of themselves.
     * Sums.  The output adds up a product for each token whose value is not zero, one or two terms each, every addition off by 2^-23 of the magnitudes;
       accumulators and sums are scaled at most once per 32 tokens (2^-24); a sum takes at most a 32nd of its tokens one after the other, and what is put together
       of threads, warps and parts is below 64 additions more.
@@ -48,6 +49,7 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
     S, H = cache.page_tokens, cache.heads
     G = HQ // H
     f32 = q.dtype == torch.float32
+    exact = bool((torch.frexp(scales[1])[0] == 0.5).all())
     terms, half = (2, 2.0 ** -22) if f32 else (1, 2.0 ** -11)
     scale = D ** -0.5 if scale is None else scale
     out = torch.full(q.shape, math.nan, dtype=F64)
@@ -84,7 +86,7 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
             nonzero = mask.double() @ (v != 0).double()
             mag = p @ v.abs()
             err = (p * eps) @ v.abs() + (p * eps).sum(1, keepdim=True) * o.abs()
-            err += (half + 2.0 ** -22) * mag
+            err += (half + 2.0 ** -22 + (0.0 if f32 or exact else 2.0 ** -11)) * mag
             err += 2.0 ** -35 * vs[:, h].max() / total.clamp(min=1.0) * (mask.double() @ vcode)
             err += 2.0 ** -31 * vs[:, h].max()
             err += (2 * terms * nonzero + count / 32 + 64) * 2.0 ** -23 * mag

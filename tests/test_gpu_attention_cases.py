@@ -88,3 +88,18 @@ def test_blocks_of_very_different_scales(R, G, D, room, dtype):
     v[..., D // 2:] *= small[:, :, None, None]
     cache.v.copy_(v.to(torch.float8_e4m3fn))
     check(normal((B, R, H * G, D), 253, TYPES[dtype]), cache, table, lengths, scale=0.25)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,G,D,room", FORMS)
+def test_scales_that_are_no_powers_of_two(R, G, D, room, dtype):
+    """A cache of the caller's own making: any positive scale."""
+    S, H, B = 32, 2, 2
+    lengths, width = [300, 97], room // S
+    table = make_table(B, width, B * width, 240)
+    cache = filled_cache(table, [n + R for n in lengths], H, S, D, B * width, 241)
+    for i, t in enumerate((cache.k_scale, cache.v_scale)):
+        t.mul_(1.0 + torch.rand(t.shape, generator=gen(242 + i)).cuda())
+    some = torch.rand(cache.v.shape, generator=gen(244)) < 3.0 / lengths[1]   # (as above: the weights and scales themselves)
+    cache.v.copy_(torch.where(some, cache.v.float().cpu().nan_to_num(0.0), torch.zeros(())).to(torch.float8_e4m3fn))
+    check(normal((B, R, H * G, D), 245, TYPES[dtype]), cache, table, lengths)
