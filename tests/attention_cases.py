@@ -1,4 +1,5 @@
-"""Attention to the paged cache in 64 bits with a bound that follows the kernels' arithmetic term by term."""
+"""Attention to the paged cache in 64 bits with a bound that follows the kernels' arithmetic term by term, and the calls that between them reach every
+kernel that cache_attention() chooses from, undivided and in parts."""
 import math
 
 import torch
@@ -94,3 +95,48 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
             out[b, :n, heads] = o.view(n, G, D)
             bound[b, :n, heads] = 1.01 * err.view(n, G, D)
     return out, bound
+
+
+# ---- which kernel a call is given to ------------------------------------------------------------------------------------
+
+def path_of(dtype, B, R, H, G, D, S, width, workspace_bytes):
+    """(kernel, rows of a unit, components, type, divided), as the call chooses: by rows, type and the room that the table has; `workspace_bytes` says
+    whether units are divided into parts."""
+    rows, room, DP = R * G, width * S, 64 if D <= 64 else 128
+    unit = 8 if rows <= 8 else 16 if rows <= 16 else 64 if rows <= 64 else 128
+    kernel = "few" if rows <= 16 else "mid" if rows <= 64 and dtype == "bf16" and room < (2048 if DP == 64 else 1024) else "wide"
+    return kernel, unit, DP, dtype, workspace_bytes > 0
+
+
+def _case(lengths, R, H, G, D, S, dtype, room, **more):
+    return dict(lengths=lengths, R=R, H=H, G=G, D=D, S=S, dtype=dtype, room=room, **more)
+
+
+def _cases():
+    out = []
+    for dtype in ("bf16", "f32"):
+        # up to 8 and up to 16 rows of a head; whole, in parts, and with room for parts that short contexts do not need
+        for D, S in ((64, 64), (48, 16), (128, 128), (112, 32)):
+            out += [_case([0, 1, 63, 300], 1, 2, 4, D, S, dtype, 384, starts=[0, 0, 60, 31]),
+                    _case([900, 3, 2500], 7, 2, 1, D, S, dtype, 2560, tree=3, counts=[7, 7, 5]),
+                    _case([0, 17, 400], 5, 1, 3, D, S, dtype, 512, counts=[5, 0, 4]),
+                    _case([1300, 40, 0], 13, 2, 1, D, S, dtype, 4096, tree=4, starts=[700, 41, 0])]
+        # 17 to 64 rows, short contexts and long ones
+        for D, S, G, R, tree in ((64, 64, 1, 61, 6), (32, 16, 3, 20, 0), (128, 64, 1, 61, 6), (96, 32, 2, 31, 3)):
+            out += [_case([0, 40, 131], R, 1, G, D, S, dtype, 256, tree=tree, starts=[0, 39, 5]),
+                    _case([700, 250, 3], R, 2, G, D, S, dtype, 896, tree=tree, counts=[R, R - 3, 1]),
+                    _case([2500, 100, 0], R, 1, G, D, S, dtype, 2688, tree=tree, starts=[1, 200, 0]),
+                    _case([90, 7] * 20 + [0], R, 8, G, D, S, dtype, 2048, tree=tree)]   # as many units as places for CTAs
+        # more than 64 rows
+        for D, S, G, R, tree in ((64, 64, 2, 61, 6), (80, 16, 1, 150, 0), (128, 128, 5, 33, 4), (16, 32, 1, 70, 0)):
+            out += [_case([0, 40, 131], R, 1, G, D, S, dtype, 384, tree=tree, starts=[0, 39, 5]),
+                    _case([1500, 250, 3], R, 1, G, D, S, dtype, 2048, tree=tree, counts=[R, R - 3, 1])]
+    return out
+
+
+CASES = _cases()
+
+
+def name_of(c):
+    more = "".join(f"-{k}" for k in ("tree", "counts", "starts") if c.get(k))
+    return f"{c['dtype']}-R{c['R']}-H{c['H']}x{c['G']}-D{c['D']}-S{c['S']}-room{c['room']}-{max(c['lengths'])}{more}"
