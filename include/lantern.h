@@ -378,8 +378,9 @@ typedef struct {
 /* Rotary positions with one to four axes (a token's index; row and column; time, height and width).
  * Pair j (0 <= j < P, P the sum of section[0..axes-1]) turns by positions[a, b, r] * inv_freq[j], a being the axis whose
  * section pair j falls in (section[0] pairs of axis 0, then section[1] pairs of axis 1, ...).  Pair j is the components
- * (2j, 2j+1) if interleaved, else (j, j+P); components from 2P on stay as they are.  Angles are formed and reduced in
- * double precision, so that far positions turn as exactly as near ones; products are fp32, rounded to dtype once.
+ * (2j, 2j+1) if interleaved, else (j, j+P); components from 2P on stay as they are.  Angles are formed and reduced as
+ * 64-bit fractions of a turn, so that far positions turn as exactly as near ones (to 2^-33 of a turn), in the same bits
+ * whichever call turns them; products are fp32, rounded to dtype once.
  *   inv_freq   [P] fp32, finite
  *   positions  [axes, B, R] int32 */
 enum { LANTERN_MAX_AXES = 4 };

@@ -328,6 +328,9 @@ __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) 
   if (s.fault || n <= 0) return;
   const int D = P.c.D, per_row = D >> 3;
   const bool rotate = P.rot.inv_freq != nullptr && which == 0;
+  uint64_t step[kMaxHeadDim / 64];   // of the pairs that this lane turns
+#pragma unroll
+  for (int e = 0; e < kMaxHeadDim / 64; ++e) step[e] = rotate && lane + 32 * e < P.rot.pairs ? turn_step(P.rot, lane + 32 * e) : 0;
   const T* x = static_cast<const T*>(P.x[which]) + b * P.xs[which].b + h * P.xs[which].h;
   const int64_t block = P.c.block(s.page, h);
   const float old = P.c.scale[which][block];
@@ -337,7 +340,11 @@ __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) 
     const T* p = x + (s.row + t) * P.xs[which].r;
     if (rotate) {
       __syncwarp();
-      for (int i = lane; i < P.rot.pairs; i += 32) angles[warp][place_of(i)] = turn(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, i);
+#pragma unroll
+      for (int e = 0; e < kMaxHeadDim / 64; ++e) {
+        const int i = lane + 32 * e;
+        if (i < P.rot.pairs) angles[warp][place_of(i)] = turn_by(step[e], position_of(P.rot, static_cast<int64_t>(b) * P.R + s.row + t, i));
+      }
       __syncwarp();
     }
     if (lane < per_row) new_values<BF16>(P, p, lane * 8, rotate ? angles[warp] : nullptr, v);

@@ -109,38 +109,33 @@ struct Rotation {
   int pairs, interleaved;
   int ends[LANTERN_MAX_AXES];   // running sums of the sections; axes that are not used end at `pairs`
 };
-// cos and sin of position * inv_freq: the product and its remainder modulo a full turn in double precision, so that the angle lies within half
-// a turn, however far the position; what rounding it to single precision leaves (at most 2^-25 half turns) turns the result once more.
-__device__ __forceinline__ float2 turn(const Rotation& R, int64_t token, int j) {
-  const int axis = (j >= R.ends[0]) + (j >= R.ends[1]) + (j >= R.ends[2]);
-  const double turns = static_cast<double>(__ldg(R.positions + axis * R.plane + token)) * static_cast<double>(__ldg(R.inv_freq + j)) *
-                       0.15915494309189533577;   // 1 / (2 pi)
-  const double halves = 2.0 * (turns - rint(turns));
-  const float near = static_cast<float>(halves), rest = static_cast<float>(halves - near) * 3.14159265f;
-  float s, c;
-  sincospif(near, &s, &c);
-  return make_float2(__fmaf_rn(-s, rest, c), __fmaf_rn(c, rest, s));
-}
-// The same where many tokens share a pair's frequency: the turns per position as a 64-bit fraction (whole turns dropped), of which a position's
-// multiple modulo one turn is an integer product.  Off by 2^-53 of the turns like the product in double precision.
+// The turns that one position stands for, as a 64-bit fraction (whole turns dropped): of a position's multiple of it, modulo one turn, an integer product
+// is exact, however far the position.  The product with 1 / (2 pi) has that number in two doubles and its own rounding beside it, so that the fraction is
+// good to its last bit and 2^31 positions to 2^-33 of a turn.
 __device__ __forceinline__ uint64_t turn_step(const Rotation& R, int j) {
-  const double turns = static_cast<double>(__ldg(R.inv_freq + j)) * 0.15915494309189533577;
-  return __double2ull_rn((turns - floor(turns)) * 18446744073709551616.0);   // (2^64 saturates: 2^-64 of a turn short)
+  constexpr double kTurns = 0.15915494309189535, kTurnsRest = -9.839338337591243e-18, kOne = 18446744073709551616.0;
+  const double f = static_cast<double>(__ldg(R.inv_freq + j)), turns = f * kTurns, rest = __fma_rn(f, kTurnsRest, __fma_rn(f, kTurns, -turns));
+  return static_cast<uint64_t>(__double2ll_rn((turns - rint(turns)) * kOne)) + static_cast<uint64_t>(__double2ll_rn((rest - rint(rest)) * kOne));
 }
+// cos and sin of a position's angle, which lies within half a turn; what rounding it to single precision leaves (at most 2^-25 half turns) turns the
+// result once more.
 __device__ __forceinline__ float2 turn_by(uint64_t step, int position) {
-  const int halves = static_cast<int>(static_cast<uint32_t>((step * static_cast<uint64_t>(static_cast<int64_t>(position))) >> 32));   // in 2^-31 half turns
+  const uint64_t angle = step * static_cast<uint64_t>(static_cast<int64_t>(position));
+  const int halves = static_cast<int>(static_cast<uint32_t>(angle >> 32));   // in 2^-31 half turns
   const float near = static_cast<float>(halves);
-  const float rest = static_cast<float>(static_cast<int>(static_cast<int64_t>(halves) - static_cast<int64_t>(near))) * (3.14159265f * 4.656612873e-10f);
+  const float rest = __fmaf_rn(static_cast<float>(static_cast<int>(static_cast<int64_t>(halves) - static_cast<int64_t>(near))), 4294967296.0f,
+                               static_cast<float>(static_cast<uint32_t>(angle))) * (3.14159265f * 1.0842021724855044e-19f);   // (2^-63)
   float s, c;
-  sincospif(near * 4.656612873e-10f, &s, &c);
+  sincospif(near * 4.656612873077393e-10f, &s, &c);   // (2^-31)
   return make_float2(__fmaf_rn(-s, rest, c), __fmaf_rn(c, rest, s));
 }
 __device__ __forceinline__ int position_of(const Rotation& R, int64_t token, int j) {
   const int axis = (j >= R.ends[0]) + (j >= R.ends[1]) + (j >= R.ends[2]);
   return __ldg(R.positions + axis * R.plane + token);
 }
+__device__ __forceinline__ float2 turn(const Rotation& R, int64_t token, int j) { return turn_by(turn_step(R, j), position_of(R, token, j)); }
 
-// The two components of a turned pair, each with one fused rounding and one of the product, so that every kernel and path gives the same bits.
+// The two components of a turned pair, each with one fused rounding and one of the product: with the angles above, every kernel and path gives the same bits.
 __device__ __forceinline__ float turned_low(float a, float b, float2 cs) { return __fmaf_rn(a, cs.x, -__fmul_rn(b, cs.y)); }
 __device__ __forceinline__ float turned_high(float a, float b, float2 cs) { return __fmaf_rn(b, cs.x, __fmul_rn(a, cs.y)); }
 
