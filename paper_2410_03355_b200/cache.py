@@ -159,6 +159,7 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, rotation: Rotation, *, inve
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_rotary: rows x [B, R, H, D] turned by positions [axes, B, R].  inverse=True turns back, which is also the gradient with
     respect to x of a gradient with respect to the result.  out: a tensor like x, or x itself; allocated if not given."""
+    inverse = bool(inverse)
     if out is None:
         with _allocating_on(stream):
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
