@@ -155,11 +155,36 @@ def _check(rc: int, where: str) -> None:
         raise LanternError(rc, where)
 
 
+class _Rotary(torch.autograd.Function):
+    """The rotation within a graph of gradients: its transpose is the rotation back."""
+
+    @staticmethod
+    def forward(ctx, x, positions, rotation, inverse):
+        if positions is None or rotation is None:
+            raise ValueError("a rotation needs positions")
+        ctx.save_for_backward(positions, rotation.inv_freq)   # (changes of them until then are noticed)
+        ctx.rotation, ctx.inverse = rotation, inverse
+        return rotary(x, positions, rotation, inverse=inverse)
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, _ = ctx.saved_tensors
+        if grad.stride(3) != 1:   # (a sum's gradient is one number expanded)
+            grad = grad.contiguous()
+        return rotary(grad, positions, ctx.rotation, inverse=not ctx.inverse), None, None, None
+
+
 def rotary(x: torch.Tensor, positions: torch.Tensor, rotation: Rotation, *, inverse: bool = False, out: Optional[torch.Tensor] = None,
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_rotary: rows x [B, R, H, D] turned by positions [axes, B, R].  inverse=True turns back, which is also the gradient with
-    respect to x of a gradient with respect to the result.  out: a tensor like x, or x itself; allocated if not given."""
+    respect to x of a gradient with respect to the result, and what backward() does where x requires a gradient.  out: a tensor like x, or x
+    itself (no gradient goes through it: refused where one is asked for); allocated if not given."""
     inverse = bool(inverse)
+    if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad):
+        if out is not None:
+            raise ValueError("out has no gradient: leave it out, or call under torch.no_grad()")
+        with _allocating_on(stream):   # (its stream is the gradient's as well)
+            return _Rotary.apply(x, positions, rotation, inverse)
     if out is None:
         with _allocating_on(stream):
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -197,7 +222,7 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, table: torch.
                  status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """lantern_cache_append: rows k, v [B, R, heads, D] become tokens lengths[b], lengths[b] + 1, ... of their sequences; keys are turned by
     positions [axes, B, R] on the way if a rotation is given.  table [B, blocks], lengths [B], counts [B] (rows that there are; None = R)
-    and status [B] (fault bits are OR-ed into it) are int32."""
+    and status [B] (fault bits are OR-ed into it) are int32.  No gradient goes through the cache: rows that require one are taken as they are."""
     if binding._call is not None and stream is None:
         rc = binding._call.append(k, v, cache._at, cache._device, table, lengths, counts, positions, None if rotation is None else rotation._at,
                                   None if rotation is None else rotation._device, status)
@@ -236,7 +261,8 @@ def cache_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, length
                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_cache_attention: queries [B, R, q_heads, D] of the rows that cache_append() has just put behind the sequences' `lengths`
     tokens, attending to the tokens from starts[b] (None: 0) on and to their own ancestors (tree_parents [B, R-1] as in verify(); None =
-    a chain, i.e. causal).  scale: None = head_dim ** -0.5.  Rows that `counts` leaves out stay as they are in `out`."""
+    a chain, i.e. causal).  scale: None = head_dim ** -0.5.  Rows that `counts` leaves out stay as they are in `out`.  The result has no
+    gradient, also where q requires one."""
     if binding._call is not None and stream is None and out is not None and workspace is not None:
         rc = binding._call.attention(q, cache._at, cache._device, table, lengths, counts, starts, tree_parents, scale, out, workspace, status)
         if rc is not None:
