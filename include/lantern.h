@@ -327,7 +327,10 @@ lantern_status lantern_verify_counts(const void* workspace, void* cuda_stream, i
  * the calling host thread's later sampling calls, the number of tries (0 = the default) and the index
  * b * (N + 1) + c of one context whose copies the fused pass deliberately never starts (-1 = none), so
  * that the path can be exercised without any fault: nothing is left in flight, the affected group
- * gives up, the rest of the call is abandoned cleanly, and the device stays usable. */
+ * gives up, the rest of the call is abandoned cleanly, and the device stays usable.
+ * lantern_cache_attention's waits (2^19 tries by default) obey the same number, and never start the copies of the
+ * tokens around token `withhold_context` of any sequence: rows of sequences that have it, and of others that the same
+ * thread block was to answer after them, are NaN, with LANTERN_ST_INTERNAL. */
 lantern_status lantern_debug_wait_test(int max_tries, int withhold_context);
 
 /* Measurement hook (not part of the method): when both arguments are non-NULL cudaEvent_t

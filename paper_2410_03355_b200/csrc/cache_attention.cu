@@ -127,6 +127,8 @@ extern "C" lantern_status lantern_cache_attention(const void* q, void* out, int 
   const int64_t qs[3] = {q_stride[0], q_stride[1], q_stride[2]};
   P.vec = aligned16(q, qs, size);
   P.scale_log2 = scale * 1.44269504088896340736f;
+  P.tries = kTries;
+  wait_test(&P.tries, &P.withhold);
   CUtensorMap km, vm;
   const int tokens = P.S < d.tile ? P.S : d.tile;
   if ((bad = code_map(&km, cache->k_code, cache, d.DP, tokens)) != LANTERN_OK || (bad = code_map(&vm, cache->v_code, cache, d.DP, tokens)) != LANTERN_OK) return bad;

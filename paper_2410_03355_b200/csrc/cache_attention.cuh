@@ -35,7 +35,14 @@ struct AttendParams {
   int least;          // tiles per part, at least
   int vec;            // query rows may be read 16 bytes at a time
   float scale_log2;   // scale * log2(e)
+  uint32_t tries;     // limit of a wait for a copy
+  int withhold;       // self-test only: the copies of the tile that holds this token are never issued (-1: none)
 };
+// The copies of a tile of TILE tokens from token0 on are withheld.
+template <int TILE>
+__device__ __forceinline__ bool withheld(const AttendParams& P, int token0) {
+  return static_cast<uint32_t>(P.withhold - token0) < static_cast<uint32_t>(TILE);
+}
 
 // What rows [m0, m0 + ROWS) of one sequence and cache head (row m: step row m / G, head m % G) have to read.
 struct Unit {
@@ -151,9 +158,10 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int 
 
 // Bounded wait for a phase without a suspension hint: with one, a thread that has to wait sleeps, and a tile's few waits in a row cost more
 // than its products.
-__device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity) {
+constexpr uint32_t kTries = 1u << 19;
+__device__ __forceinline__ bool await(const AttendParams& P, uint64_t* bar, uint32_t parity) {
   const uint32_t a = smem_addr(bar);
-  for (uint32_t i = 0; i < (1u << 19); ++i) {
+  for (uint32_t i = 0; i < P.tries; ++i) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -193,6 +201,9 @@ __device__ __forceinline__ Box look_up(const AttendParams& P, const Unit& u, int
   }
   return x;
 }
+// Host: what lantern_debug_wait_test has set for this thread (verify.cu); `tries` stays where that is nothing.
+void wait_test(uint32_t* tries, int* withhold);
+
 // Host: how a call's rows and tokens are divided.
 struct Division {
   enum { kFew, kMid, kWide } kernel;

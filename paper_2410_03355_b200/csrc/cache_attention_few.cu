@@ -99,12 +99,13 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
       if (i + batch < tiles) next = look_up<kTile>(P, u, u.lo + warp + kWarps * (i + batch + my_tile), my_sub, u.hi, found);
     }
     const bool turn = my_tile == in_batch, mine = turn && box.mine;
+    const int token0 = (u.tile0 + u.lo + warp + kWarps * i) * kTile;
     const int copies = __popc(__ballot_sync(kFull, mine));   // (at least one: every tile has a token that some row sees)
     if (lane == 0) mbar_expect_tx(&full[stage], copies * 2 * sub * DP);
     __syncwarp();
-    if (mine) {
+    if (mine && !withheld<kTile>(P, token0)) {
       uint8_t* at = stages + stage * kStageBytes + my_sub * DP;
-      const int row = u.h * P.S + ((u.tile0 + u.lo + warp + kWarps * i) * kTile + my_sub) % P.S;
+      const int row = u.h * P.S + (token0 + my_sub) % P.S;
       tma_load(at, &kmap, row, box.page, &full[stage]);
       tma_load(at + kTile * DP, &vmap, row, box.page, &full[stage]);
     }
@@ -202,8 +203,11 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
 
   for (int i = 0; i < tiles; ++i) {
     const int stage = i % STAGES;
-    ok = ok && await(&full[stage], (i / STAGES) & 1);
-    __syncwarp();
+    ok = __all_sync(kFull, await(P, &full[stage], (i / STAGES) & 1));
+    if (!ok) {   // nothing may be under way into the stages when they are used for something else, or when the CTA ends
+      for (int k = i; k < min(i + STAGES, tiles); ++k) await(P, &full[k % STAGES], (k / STAGES) & 1);
+      break;
+    }
     const uint8_t *keys = stages + stage * kStageBytes, *values = keys + kTile * DP;
     const int token0 = (u.tile0 + u.lo + warp + kWarps * i) * kTile;
     const bool edge = token0 < u.begin || token0 + kTile > u.len + (P.parents ? 0 : 1);   // some row may not see all of the tile

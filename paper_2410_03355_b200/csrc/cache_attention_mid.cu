@@ -131,9 +131,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
     const int copies = __popc(__ballot_sync(kFull, mine));   // (at least one: every tile has a token that some row sees)
     if (lane == 0) mbar_expect_tx(&S.full[stage], copies * 2 * sub * DP);
     __syncwarp();
-    if (mine) {
+    const int token0 = (u.tile0 + u.lo + i) * kTile;
+    if (mine && !withheld<kTile>(P, token0)) {
       uint8_t* at = smem + (stage * 2 * kTile + my_sub) * DP;
-      const int row = u.h * P.S + ((u.tile0 + u.lo + i) * kTile + my_sub) % P.S;
+      const int row = u.h * P.S + (token0 + my_sub) % P.S;
       tma_load(at, &kmap, row, box.page, &S.full[stage]);
       tma_load(at + kTile * DP, &vmap, row, box.page, &S.full[stage]);
     }
@@ -208,6 +209,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   float vref = 0.0f, v_over = 0.0f;   // largest value scale met (roughly) and its reciprocal
   const uint32_t base = smem_addr(halves);
   bool ok = true;
+  int converted = 0;   // tiles that this warp has waited for
 
   // Offsets of a lane's 16 bytes: of its token's codes (chunk lane / QUARTER; the j-th of its chunks lies at an exclusive or with j << kCodeStep), of the
   // halves that they become (j << kHalfStep, second half 16), and of its ldmatrix rows (keys: step s at s << 5; values: column tiles n, n + 1 at n << 4).  Whole groups of eight
@@ -224,8 +226,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   // this warp's quarter of tile i as halves
   auto convert = [&](int i) {
     const int stage = i % kStages, k = i & 1;
-    ok = ok && await(&S.full[stage], (i / kStages) & 1);
-    __syncwarp();
+    ok = ok && __all_sync(kFull, await(P, &S.full[stage], (i / kStages) & 1));
+    converted += ok;
     const uint8_t* raw = smem + stage * kRaw;
     uint8_t* to = halves + 2 * k * kHalves;
     const bool edge = edge_of(i);
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   if (tiles > 0) convert(0);
   __syncthreads();
   for (int i = 0; i < tiles; ++i) {
-    if (warp == 0 && i + kStages < tiles) ask(i + kStages);   // (into the stage that tile i has been taken from)
+    if (warp == 0 && ok && i + kStages < tiles) ask(i + kStages);   // (into the stage that tile i has been taken from)
     if (i + 1 < tiles) convert(i + 1);
     float ks[SG], vs[SG];
 #pragma unroll
@@ -396,7 +398,11 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
     sum[half] += __shfl_xor_sync(kFull, sum[half], 1);
     sum[half] += __shfl_xor_sync(kFull, sum[half], 2);
   }
-  if (!ok) found |= LANTERN_ST_INTERNAL;
+  if (!ok) {
+    found |= LANTERN_ST_INTERNAL;
+    if (warp == 0)   // nothing may be under way when the CTA ends: tiles up to kStages behind the last that came have been asked for
+      for (int i = converted; i < min(converted + kStages, tiles); ++i) await(P, &S.full[i % kStages], (i / kStages) & 1);
+  }
   if (found) atomicOr(&S.fault, found);
   __syncthreads();
   const int fault = S.fault;

@@ -47,7 +47,7 @@ template <int DP>
 struct WideShared {
   static constexpr int kTile = Shape<DP>::kTile, kStages = Shape<DP>::kStages;
   uint64_t full[kStages], empty[kStages];
-  uint64_t keys_full[2], keys_free[2], values_full[2], values_free[2], scores_full[2], probs_full[2], query_full;
+  uint64_t keys_full[2], keys_free[2], values_full[2], values_free[2], scores_full[2], probs_full[2], query_full, given_up;
   float scale[kStages][2][kTile / 16];   // of every 16 tokens: keys; values, over the largest of the part, lifted
   int flags[kStages];                    // of a stage's tile
   float key_scale[4][kTile / 16];        // of the tiles whose scores are under way
@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       mbar_init(&S.probs_full[i], 4);
     }
     mbar_init(&S.query_full, 4);
+    mbar_init(&S.given_up, 1);
     fence_mbar_init();
   }
   if (warp == 9) {
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
           if (i + batch < tiles) fault |= late;
         }
         const int stage = n % STAGES;
-        ok = n < STAGES || await(&S.empty[stage], ((n / STAGES) - 1) & 1);
+        ok = n < STAGES || await(P, &S.empty[stage], ((n / STAGES) - 1) & 1);
         ok = __all_sync(kFull, ok);
         if (!ok) break;
         const bool turn = my_stage == in_batch, mine = turn && x.mine;
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
           mbar_expect_tx(&S.full[stage], copies * 2 * sub * DP);
         }
         __syncwarp();
-        if (mine) {
+        if (mine && !withheld<TILE>(P, token0)) {
           uint8_t* at = smem + (stage * 2 * TILE + my_sub) * DP;
           const int row = u.h * P.S + (token0 + my_sub) % P.S;
           tma_load(at, &kmap, row, x.page, &S.full[stage]);
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
     // no more: a stage without copies says so; and nothing may be in flight when the CTA ends
     if (ok) {
       const int stage = n % STAGES;
-      ok = n < STAGES || await(&S.empty[stage], ((n / STAGES) - 1) & 1);
+      ok = n < STAGES || await(P, &S.empty[stage], ((n / STAGES) - 1) & 1);
       ok = __all_sync(kFull, ok);
       if (ok && lane == 0) {
         S.flags[stage] = kEnd;
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       }
     }
     // (the tile that was in the last stage before has been read: its barrier has gone on)
-    for (int i = max(0, n - STAGES + (ok ? 1 : 0)); i < n; ++i) await(&S.full[i % STAGES], (i / STAGES) & 1);
+    for (int i = max(0, n - STAGES + (ok ? 1 : 0)); i < n; ++i) await(P, &S.full[i % STAGES], (i / STAGES) & 1);
     __syncwarp();
   } else if (warp == 9) {   // ---- products ----
     if (lane == 0) {
@@ -307,13 +308,13 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       bool ok = true;
       int units = 0;
       auto flags_of = [&](int n) {   // waits for the tile's keys
-        ok = ok && await(&S.keys_full[n & 1], (n >> 1) & 1);
+        ok = ok && await(P, &S.keys_full[n & 1], (n >> 1) & 1);
         return ok ? S.tile_flags[n & 3] : static_cast<int>(kEnd);
       };
       auto scores = [&](int n, int flags) {
         const int k = n & 1;
         if (flags & kFirst) {
-          ok = ok && await(&S.query_full, units & 1);
+          ok = ok && await(P, &S.query_full, units & 1);
           ++units;
         }
         tmem_fence_after();
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         const int k = n & 1, coming = flags_of(n + 1);
         // the next tile's scores go ahead of this one's output, unless they have to wait for the next unit's queries
         if (!(coming & (kEnd | kFirst))) scores(n + 1, coming);
-        ok = ok && await(&S.probs_full[k], (n >> 1) & 1) && await(&S.values_full[k], (n >> 1) & 1);
+        ok = ok && await(P, &S.probs_full[k], (n >> 1) & 1) && await(P, &S.values_full[k], (n >> 1) & 1);
         tmem_fence_after();
 #pragma unroll
         for (int s = 0; s < TILE / 16; ++s)
@@ -344,6 +345,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
         commit(&S.values_free[k]);
         if (coming & kFirst) scores(n + 1, coming);
         flags = coming;
+      }
+      if (!ok) {   // (a wait ran out, and nobody waits for what has been issued: it ends before the tensor memory is given back)
+        commit(&S.given_up);
+        await(P, &S.given_up, 0);
       }
     }
     __syncwarp();
@@ -356,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
     bool ok = true;
     for (int n = 0; ok; ++n) {
       const int k = n & 1, stage = n % STAGES, at = n & 3;
-      ok = await(&S.full[stage], (n / STAGES) & 1);
+      ok = await(P, &S.full[stage], (n / STAGES) & 1);
       ok = __all_sync(kFull, ok);
       if (!ok) break;
       const int flags = S.flags[stage];
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       bool nan = false;
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
-        if (n >= 2) ok = ok && await(which ? &S.values_free[k] : &S.keys_free[k], ((n >> 1) - 1) & 1);
+        if (n >= 2) ok = ok && await(P, which ? &S.values_free[k] : &S.keys_free[k], ((n >> 1) - 1) & 1);
         uint8_t* out = halves + (k * 2 + which) * C::kHalves;
 #pragma unroll 2
         for (int c = 0; c < CHUNKS; ++c) {
@@ -571,10 +576,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       float ref = -INFINITY, sum = 0.0f;
       for (int i = 0; i < tiles && ok; ++i, ++n) {
         const int k = n & 1;
-        ok = await(&S.scores_full[k], (n >> 1) & 1);
+        ok = await(P, &S.scores_full[k], (n >> 1) & 1);
         const int token0 = (u.tile0 + u.lo + i) * TILE;
         const bool edge = S.tile_flags[n & 3] & kEdge;
-        if (edge) ok = ok && await(&S.values_full[k], (n >> 1) & 1);
+        if (edge) ok = ok && await(P, &S.values_full[k], (n >> 1) & 1);
         __syncwarp();
         tmem_fence_after();
         auto factors = [&](int j, float& fa, float& fb) {   // of the two sixteens of run j of this thread's
@@ -632,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
           ref = to;
           sum *= w;
           if (i > 0) {
-            ok = ok && await(&S.values_free[(n - 1) & 1], ((n - 1) >> 1) & 1);
+            ok = ok && await(P, &S.values_free[(n - 1) & 1], ((n - 1) >> 1) & 1);
             __syncwarp();
             tmem_fence_after();
 #pragma unroll 1
@@ -693,10 +698,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
       }
       if (more && v.lo < v.hi && ok) put_queries(v);   // the next unit's scores can begin
       if (tiles > 0) {
-        ok = ok && await(&S.values_free[(n - 1) & 1], ((n - 1) >> 1) & 1);
+        ok = ok && await(P, &S.values_free[(n - 1) & 1], ((n - 1) >> 1) & 1);
         __syncwarp();
         tmem_fence_after();
-        fault |= S.fault[slot & (kSlots - 1)];
+        if (ok) fault |= S.fault[slot & (kSlots - 1)];
       }
       if (!ok) fault |= LANTERN_ST_INTERNAL;
       if (fault && tid == 0 && P.status) atomicOr(P.status + u.b, fault);

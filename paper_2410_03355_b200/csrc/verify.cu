@@ -511,6 +511,11 @@ static thread_local cudaEvent_t g_ev_before = nullptr, g_ev_after = nullptr;
 constexpr uint32_t kDefaultWaitTries = 1u << 21;
 static thread_local uint32_t g_wait_tries = kDefaultWaitTries;
 static thread_local int g_withhold_item = -1;
+void wait_test(uint32_t* tries, int* withhold);   // (of the attention kernels as well, whose limit is one of their own if none is set)
+void wait_test(uint32_t* tries, int* withhold) {
+  if (g_wait_tries != kDefaultWaitTries) *tries = g_wait_tries;
+  *withhold = g_withhold_item;
+}
 
 // the variants of the fused context kernel live in verify_context_v<tone + 2 jsd + 4 topk>.cu, those of greedy decoding in
 // verify_context_v<8 + jsd + 2 topk>.cu
