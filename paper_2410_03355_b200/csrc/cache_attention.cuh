@@ -175,6 +175,35 @@ __device__ __forceinline__ bool await(const AttendParams& P, uint64_t* bar, uint
   return false;
 }
 
+// ---- halves, NaN codes, bits ----
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t rounded) {   // what the rounding left
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
+  return half2_of(lo - f.x, hi - f.y);
+}
+__device__ __forceinline__ uint32_t without_nan(uint32_t codes) { return codes & ~__vcmpeq4(codes & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+__device__ __forceinline__ bool has_nan(uint4 x) {
+  return ((__vcmpeq4(x.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.y & 0x7f7f7f7fu, 0x7f7f7f7fu)) |
+          (__vcmpeq4(x.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.w & 0x7f7f7f7fu, 0x7f7f7f7fu))) != 0;
+}
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// A query row's halves are its components times `mult`, which takes the largest of them (`most`) to [2^14, 2^15) and has the scale's sign, so that `factor`,
+// what the products come back with, is positive.  odd: a component is not finite.
+struct QueryPower {
+  float mult, factor;
+};
+__device__ __forceinline__ QueryPower query_power(const AttendParams& P, float most, bool odd) {
+  const int up = min(268 - static_cast<int>(__float_as_uint(most) >> 23), 254);   // biased exponent of the multiplier
+  float mult = most == 0.0f || odd || P.scale_log2 == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(up) << 23);
+  if (P.scale_log2 < 0.0f) mult = -mult;
+  return {mult, odd ? __int_as_float(0x7fffffff) : ldexpf(fabsf(P.scale_log2), 127 - up)};
+}
+
 // byte offset of a 16-byte chunk of a token's codes within a stage's keys or values, as the swizzled copy leaves it
 template <int DP>
 __device__ __forceinline__ int chunk_at(int token, int chunk) {

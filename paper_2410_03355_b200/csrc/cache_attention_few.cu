@@ -41,22 +41,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of 8 by 8 halv
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t rounded) {   // what the rounding left
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
-  return half2_of(lo - f.x, hi - f.y);
-}
 __device__ __forceinline__ uint32_t low2(uint32_t w) { return decode2(static_cast<uint16_t>(w & 0xffffu)); }
 __device__ __forceinline__ uint32_t high2(uint32_t w) { return decode2(static_cast<uint16_t>(w >> 16)); }
-__device__ __forceinline__ uint32_t without_nan(uint32_t codes) { return codes & ~__vcmpeq4(codes & 0x7f7f7f7fu, 0x7f7f7f7fu); }
-__device__ __forceinline__ bool has_nan(uint4 x) {
-  return ((__vcmpeq4(x.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.y & 0x7f7f7f7fu, 0x7f7f7f7fu)) |
-          (__vcmpeq4(x.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.w & 0x7f7f7f7fu, 0x7f7f7f7fu))) != 0;
-}
 
 // NQ: eights of rows.
 template <int NQ, int DP, bool BF16>
@@ -76,7 +62,6 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
   const Unit u = unit_of(P, ROWS, kTile, unit, static_cast<int>(blockIdx.x - unit * P.splits), unit_in(P, unit));
   grid_dependents_launch();
   if (!u.rows || u.split >= u.parts) return;
-  const int words = (P.R + 31) >> 5, table_rows = (ROWS + P.G - 1) / P.G + 1;   // (a unit is all rows there are: its first is row 0)
   uint8_t* stages = smem + warp * STAGES * kStageBytes;
   uint64_t* full = S.full[warp];
   if (tid == 0) S.fault = u.fault;
@@ -149,11 +134,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
     most = fmaxf(most, __shfl_xor_sync(kFull, most, 2));
     odd |= __shfl_xor_sync(kFull, odd, 1);
     odd |= __shfl_xor_sync(kFull, odd, 2);
-    // largest component to [2^14, 2^15); the scale's sign goes with the query, so that factors are positive
-    const int up = min(268 - static_cast<int>(__float_as_uint(most) >> 23), 254);   // biased exponent of the multiplier
-    float mult = most == 0.0f || odd || P.scale_log2 == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(up) << 23);
-    if (P.scale_log2 < 0.0f) mult = -mult;
-    const float f = odd ? __int_as_float(0x7fffffff) : ldexpf(fabsf(P.scale_log2), 127 - up);
+    const QueryPower power = query_power(P, most, odd);
+    const float mult = power.mult, f = power.factor;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -171,20 +153,21 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
   }
   if (P.parents && !u.fault) {
     const int32_t* parents = P.parents + static_cast<int64_t>(u.b) * (P.R - 1);
-    int32_t* nodes = reinterpret_cast<int32_t*>(bits + table_rows * words);
+    int32_t* nodes = reinterpret_cast<int32_t*>(bits + ROWS);   // (a unit is all rows there are, 16 at most: a word of bits each)
     __syncthreads();   // (the fault word is there)
-    for (int i = tid; i < u.n - 1; i += kThreads) {
-      const int p = __ldg(parents + i);
-      nodes[i] = p;
-      if (p < -1 || p >= i) atomicOr(&S.fault, LANTERN_ST_BAD_PARENT);
+    if (tid < u.n - 1) {
+      const int p = __ldg(parents + tid);
+      nodes[tid] = p;
+      if (p < -1 || p >= tid) atomicOr(&S.fault, LANTERN_ST_BAD_PARENT);
     }
-    for (int i = tid; i < table_rows * words; i += kThreads) bits[i] = 0;
     __syncthreads();
-    const bool ok = !(S.fault & LANTERN_ST_BAD_PARENT);
-    for (int i = tid; i < table_rows && i < u.n && ok; i += kThreads) {
-      uint32_t* mine = bits + i * words;
-      for (int r = i; r > 0; r = nodes[r - 1] + 1) mine[r >> 5] |= 1u << (r & 31);
-      mine[0] |= 1u;
+    if (tid < u.n) {
+      uint32_t mine = 0u;
+      if (!(S.fault & LANTERN_ST_BAD_PARENT)) {
+        for (int r = tid; r > 0; r = nodes[r - 1] + 1) mine |= 1u << r;
+        mine |= 1u;
+      }
+      bits[tid] = mine;
     }
     __syncthreads();
   }
@@ -249,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 && BF16 ? 3 : 2) lantern_att
           for (int e = 0; e < 4; ++e) {
             const int at = 16 * k + 8 * (e >> 1) + g, token = token0 + at, r = row_of[q][e & 1], ahead = token - u.len;
             bool see = r >= 0 && token >= u.begin && token < u.end;
-            if (see && ahead >= 0) see = P.parents ? (bits[r * words + (ahead >> 5)] >> (ahead & 31)) & 1u : ahead <= r;
+            if (see && ahead >= 0) see = P.parents ? (bits[r] >> ahead) & 1u : ahead <= r;
             if (!see) c[k][q][e] = -INFINITY;
             else if ((bad >> at) & 1u) c[k][q][e] = __int_as_float(0x7fffffff);
           }
@@ -410,10 +393,9 @@ template <int NQ, int DP, bool BF16>
 cudaError_t launch(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, cudaStream_t st) {
   constexpr size_t kFixed = kWarps * kStagesOf<DP> * 2 * kTile * DP + sizeof(FewShared<16>);
   static_assert(kWarps * 8 * NQ * (DP + 4) * sizeof(float) <= kWarps * kStagesOf<DP> * 2 * kTile * DP, "accumulators");
-  const size_t words = (P.R + 31) / 32, rows = (16 + P.G - 1) / P.G + 1;
-  const size_t smem = kFixed + (P.parents ? (rows * words + P.R) * 4 : 0);
+  const size_t smem = kFixed + (P.parents ? 2 * 16 * 4 : 0);   // (a word of bits and a parent for each row)
   static DeviceFlags ready;
-  cudaError_t e = allow_shared_memory(lantern_attention_few_kernel<NQ, DP, BF16>, kFixed + (17 + 16) * 4, ready);   // (at most 16 rows: one word each)
+  cudaError_t e = allow_shared_memory(lantern_attention_few_kernel<NQ, DP, BF16>, kFixed + 2 * 16 * 4, ready);
   if (e != cudaSuccess) return e;
   lantern_attention_few_kernel<NQ, DP, BF16><<<static_cast<unsigned>(d.units * d.splits), kThreads, smem, st>>>(P, k, v);
   if ((e = cudaGetLastError()) != cudaSuccess || d.splits == 1) return e;

@@ -41,17 +41,6 @@ __device__ __forceinline__ void load4(uint32_t (&r)[4], uint32_t at) {
 __device__ __forceinline__ void load4_across(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t without_nan(uint32_t codes) { return codes & ~__vcmpeq4(codes & 0x7f7f7f7fu, 0x7f7f7f7fu); }
-__device__ __forceinline__ bool has_nan(uint4 x) {
-  return ((__vcmpeq4(x.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.y & 0x7f7f7f7fu, 0x7f7f7f7fu)) |
-          (__vcmpeq4(x.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.w & 0x7f7f7f7fu, 0x7f7f7f7fu))) != 0;
-}
-__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 // byte offset of 16 bytes of a token's halves: `unit` counts them along the row, 128-byte runs swizzled
 template <int DP>
 __device__ __forceinline__ int half_at(int token, int unit) {
@@ -81,7 +70,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   uint32_t raw[2][KS][2];   // pairs of components 16 s + 2 t and 8 further
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const int m = u.m0 + warp * 16 + g + 8 * half, r = m / P.G;
+    const int m = warp * 16 + g + 8 * half, r = m / P.G;   // (a unit is all rows there are: its first is row 0)
     row_of[half] = r < u.n ? r : -1;
     const T* p = static_cast<const T*>(P.q) + u.b * P.qs.b + r * P.qs.r + (static_cast<int64_t>(u.h) * P.G + (m - r * P.G)) * P.qs.h;
     if (P.vec) {
@@ -106,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   }
   const int32_t* parents = P.parents && !u.fault ? P.parents + static_cast<int64_t>(u.b) * (P.R - 1) : nullptr;
   const int parent = parents && tid < u.n - 1 ? __ldg(parents + tid) : -1;
-  const int words = (P.R + 31) >> 5, first_row = u.m0 / P.G, table_rows = (kRows + P.G - 1) / P.G + 1;
+  const int words = (P.R + 31) >> 5;   // (1 or 2)
   if (tid == 0) {
     S.fault = u.fault;
     for (int i = 0; i < kStages; ++i) mbar_init(&S.full[i], 1);
@@ -168,11 +157,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
       most = fmaxf(most, __shfl_xor_sync(kFull, most, 2));
       odd |= __shfl_xor_sync(kFull, odd, 1);
       odd |= __shfl_xor_sync(kFull, odd, 2);
-      // largest component to [2^14, 2^15); the scale's sign goes with the query, so that factors are positive
-      const int up = min(268 - static_cast<int>(__float_as_uint(most) >> 23), 254);   // biased exponent of the multiplier
-      float mult = most == 0.0f || odd || P.scale_log2 == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(up) << 23);
-      if (P.scale_log2 < 0.0f) mult = -mult;
-      factor[half] = odd ? __int_as_float(0x7fffffff) : ldexpf(fabsf(P.scale_log2), 127 - up);
+      const QueryPower power = query_power(P, most, odd);
+      const float mult = power.mult;
+      factor[half] = power.factor;
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -184,20 +171,16 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
     }
   }
   if (parents) {
-    int32_t* nodes = reinterpret_cast<int32_t*>(bits + table_rows * words);
-    for (int i = tid; i < u.n - 1; i += 128) {
-      const int p = i < 128 ? parent : __ldg(parents + i);
-      nodes[i] = p;
-      if (p < -1 || p >= i) atomicOr(&S.fault, LANTERN_ST_BAD_PARENT);
+    int32_t* nodes = reinterpret_cast<int32_t*>(bits + P.R * words);
+    if (tid < u.n - 1) {
+      nodes[tid] = parent;
+      if (parent < -1 || parent >= tid) atomicOr(&S.fault, LANTERN_ST_BAD_PARENT);
     }
-    for (int i = tid; i < table_rows * words; i += 128) bits[i] = 0;
+    if (tid < P.R * words) bits[tid] = 0;
     __syncthreads();
-    const bool ok = !(S.fault & LANTERN_ST_BAD_PARENT);
-    for (int i = tid; i < table_rows && ok; i += 128) {
-      int r = first_row + i;
-      if (r >= u.n) break;
-      uint32_t* mine = bits + i * words;
-      for (; r > 0; r = nodes[r - 1] + 1) mine[r >> 5] |= 1u << (r & 31);
+    if (tid < u.n && !(S.fault & LANTERN_ST_BAD_PARENT)) {
+      uint32_t* mine = bits + tid * words;
+      for (int r = tid; r > 0; r = nodes[r - 1] + 1) mine[r >> 5] |= 1u << (r & 31);
       mine[0] |= 1u;
     }
   }
@@ -221,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
 
   auto edge_of = [&](int i) {
     const int token0 = (u.tile0 + u.lo + i) * kTile;
-    return token0 < u.begin || token0 + kTile > u.len + (P.parents ? 0 : first_row + 1);   // some row may not see all of the tile
+    return token0 < u.begin || token0 + kTile > u.len + (P.parents ? 0 : 1);   // some row may not see all of the tile
   };
   // this warp's quarter of tile i as halves
   auto convert = [&](int i) {
@@ -285,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int r = row_of[half];
-        const uint32_t* seen = bits + (r < 0 ? 0 : r - first_row) * words;
+        const uint32_t* seen = bits + (r < 0 ? 0 : r) * words;
 #pragma unroll
         for (int w = 0; w < kTile / 32; ++w) {
           const int a = token0 + 32 * w, ahead = a - u.len;
@@ -413,8 +396,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
   for (int half = 0; half < 2; ++half) {
     const int row = warp * 16 + g + 8 * half, r = row_of[half];
     if (r < 0) continue;
-    const int m = u.m0 + row;
-    T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (m - r * P.G)) * P.D;
+    T* out = static_cast<T*>(P.out) + ((static_cast<int64_t>(u.b) * P.R + r) * P.q_heads + u.h * P.G + (row - r * P.G)) * P.D;
     float* to = P.parts + (part + row) * DP;
     const float own = vref * (1.0f / kLift);
     const float scale = fault ? __int_as_float(0x7fffffff) : whole ? (sum[half] == 0.0f ? 0.0f : own / sum[half]) : own;
@@ -434,10 +416,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) lantern_attention_
 template <int DP>
 cudaError_t launch(const AttendParams& P, const CUtensorMap& k, const CUtensorMap& v, const Division& d, cudaStream_t st) {
   constexpr size_t kFixed = (kStages * 2 + 8) * kTileOf<DP> * DP + sizeof(MidShared);
-  const size_t words = (P.R + 31) / 32, rows = (kRows + P.G - 1) / P.G + 1;
-  const size_t smem = kFixed + (P.parents ? (rows * words + P.R) * 4 : 0);
+  const size_t smem = kFixed + (P.parents ? (P.R * ((P.R + 31) / 32) + P.R) * 4 : 0);
   static DeviceFlags ready;
-  cudaError_t e = allow_shared_memory(lantern_attention_mid_kernel<DP>, kFixed + ((kRows + 1) * 33 + kMaxTreeRows) * 4, ready);
+  cudaError_t e = allow_shared_memory(lantern_attention_mid_kernel<DP>, kFixed + (kRows * 2 + kRows) * 4, ready);   // (at most 64 rows)
   if (e != cudaSuccess) return e;
   lantern_attention_mid_kernel<DP><<<static_cast<unsigned>(d.units * d.splits), kThreads, smem, st>>>(P, k, v);
   if ((e = cudaGetLastError()) != cudaSuccess || d.splits == 1) return e;

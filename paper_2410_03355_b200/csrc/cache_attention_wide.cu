@@ -112,20 +112,6 @@ __device__ __forceinline__ void commit(uint64_t* bar) {   // arrives when the pr
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
-__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t rounded) {   // what the rounding left
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
-  return half2_of(lo - f.x, hi - f.y);
-}
-__device__ __forceinline__ uint32_t without_nan(uint32_t codes) { return codes & ~__vcmpeq4(codes & 0x7f7f7f7fu, 0x7f7f7f7fu); }
-__device__ __forceinline__ bool has_nan(uint4 x) {
-  return ((__vcmpeq4(x.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.y & 0x7f7f7f7fu, 0x7f7f7f7fu)) |
-          (__vcmpeq4(x.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(x.w & 0x7f7f7f7fu, 0x7f7f7f7fu))) != 0;
-}
 __device__ __forceinline__ uint32_t times(uint32_t halves, __half2 ratio) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&halves), ratio);
   return *reinterpret_cast<const uint32_t*>(&r);
@@ -136,7 +122,6 @@ __device__ __forceinline__ float power_of(float x) {
   return (b & 0x7f800000u) == 0x7f800000u ? x : __uint_as_float(b & 0xff800000u);
 }
 __device__ __forceinline__ float digits_of(float x) { return __uint_as_float((__float_as_uint(x) & 0x7fffffu) | 0x3f800000u); }
-__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 __device__ __forceinline__ void rows_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }   // of the softmax warps
 __device__ __forceinline__ bool rows_any(bool x) {
@@ -483,11 +468,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) lantern_attention_
           }
         }
       }
-      // largest component to [2^14, 2^15); the scale's sign goes with the query, so that factors are positive
-      const int up = min(268 - static_cast<int>(__float_as_uint(most) >> 23), 254);   // biased exponent of the multiplier
-      float mult = most == 0.0f || odd || P.scale_log2 == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(up) << 23);
-      if (P.scale_log2 < 0.0f) mult = -mult;
-      factor = odd ? __int_as_float(0x7fffffff) : ldexpf(fabsf(P.scale_log2), 127 - up);
+      const QueryPower power = query_power(P, most, odd);
+      const float mult = power.mult;
+      factor = power.factor;
 #pragma unroll 1
       for (int run = 0; run < RUNS; ++run) {
         if (RUNS > 1) fetch(run);
