@@ -465,8 +465,8 @@ lantern_status lantern_cache_keep(const lantern_cache* cache, const int32_t* tab
                                   int N, int32_t* out_lengths, int32_t* status, void* cuda_stream);
 
 /* Reads tokens first[b] .. first[b] + counts[b] - 1 back (counts NULL: R of them).
- *   out_k, out_v  [B, R, heads, D] contiguous, dtype; 16-byte aligned.  With a fault (BAD_LENGTH: any of the tokens lies
- *                 outside the table; BAD_BLOCK) the rows concerned are NaN */
+ *   out_k, out_v  [B, R, heads, D] contiguous, dtype; 16-byte aligned.  With BAD_LENGTH (any of the tokens lies
+ *                 outside the table) all R rows of the sequence are NaN, with BAD_BLOCK those of the block */
 lantern_status lantern_cache_read(const lantern_cache* cache, const int32_t* table, int table_width,
                                   const int32_t* first, const int32_t* counts, int B, int R, int dtype, void* out_k,
                                   void* out_v, int32_t* status, void* cuda_stream);

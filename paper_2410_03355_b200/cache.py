@@ -177,8 +177,8 @@ class _Rotary(torch.autograd.Function):
 def rotary(x: torch.Tensor, positions: torch.Tensor, rotation: Rotation, *, inverse: bool = False, out: Optional[torch.Tensor] = None,
            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """lantern_rotary: rows x [B, R, H, D] turned by positions [axes, B, R].  inverse=True turns back, which is also the gradient with
-    respect to x of a gradient with respect to the result, and what backward() does where x requires a gradient.  out: a tensor like x, or x
-    itself (no gradient goes through it: refused where one is asked for); allocated if not given."""
+    respect to x of a gradient with respect to the result, and what backward() does where x requires a gradient (positions and frequencies
+    have none).  out: a tensor like x, or x itself (no gradient goes through it: refused where one is asked for); allocated if not given."""
     inverse = bool(inverse)
     if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad):
         if out is not None:

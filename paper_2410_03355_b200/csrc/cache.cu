@@ -211,8 +211,8 @@ __device__ __forceinline__ float new_scale(float amax, float old, bool held, int
 
 // A CTA per touched block, run of heads and kind (keys or values): a block's angles are formed once for the heads of the run, then every head goes through
 // registers, U units of eight components per thread: maximum over the block, scale, codes.  Bound by the latency of a head's reads, the
-// maximum and the writes one after the other, and (keys) by the angles' arithmetic (32 prompts of 0 to 1024 rows, 8 heads of 128: 47 us for 100 MB,
-// 33 without rotation; 53 with the angles in their order, eight threads to a bank; with angles formed in double precision and a read at a time 81;
+// maximum and the writes one after the other, and (keys) by the angles' arithmetic (32 prompts of 0 to 1024 rows, 8 heads of 128: 58 us for 100 MB;
+// of rows that L2 holds 48, 33 without rotation, 53 with the angles in their order, eight threads to a bank; with angles formed in double precision and a read at a time 81;
 // both kinds in one CTA 69; the next head's reads under way ahead of this one's maximum: fp32 blocks of 32 tokens 74 -> 82 with the read, for registers).
 template <bool BF16, int AT, int U>   // AT threads
 __global__ void __launch_bounds__(AT, (U == 1 ? 5 : U == 2 ? 4 : 2) * 256 / AT) lantern_append_kernel(AppendParams P) {
@@ -311,7 +311,8 @@ __global__ void __launch_bounds__(AT, (U == 1 ? 5 : U == 2 ? 4 : 2) * 256 / AT) 
 }
 
 // Few rows a sequence: a warp per touched block, head and kind.  The rows are read twice (the second time from L1); angles are formed by the
-// lane that needs them.  Bound by latency (128 sequences of one row, 8 heads: 6 us, most of it the launch).
+// lane that needs them.  Bound by latency: 128 sequences of one row, 8 heads of 128: 6.6 us, most of it the launch, where the blocks' scales stay; 14.5 where all
+// grow and 32 held tokens of a block on average are coded anew, 8 bytes a lane at a time (21 with blocks of 128 tokens).
 constexpr int FT = 128;
 template <bool BF16>
 __global__ void __launch_bounds__(FT) lantern_append_few_kernel(AppendParams P) {
@@ -391,7 +392,7 @@ struct KeepParams {
 
 // A warp per sequence, head and kind.  Targets ascend and no target lies behind its source (a path is increasing), so that going through the
 // targets in order, block by block, never overwrites a source that is still needed.  Bound by latency: accepted path, table, scale, code one after the
-// other (256 trees, 20 heads: 11 us).
+// other (256 trees, 20 heads: 16 us with nothing in L2).
 constexpr int KT = 128;
 __global__ void __launch_bounds__(KT) lantern_keep_kernel(KeepParams P) {
   const int lane = threadIdx.x & 31;
@@ -575,6 +576,8 @@ extern "C" lantern_status lantern_cache_append(const void* k, const void* v, int
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool bf = dtype == LANTERN_BF16;
   cudaError_t e;
+  // Up to 4 rows a warp per block, head and kind, else a CTA per block and run of heads (8 heads of 128, with the read: 128 sequences of 1 row 17 us, by CTAs
+  // 32; of 4 rows 24 and 31; of 5 26 and 31, of 8 31 and 33, of 16 47 and 37.  2 sequences of 1 row 9.3 and 10.3, of 4 13.7 and 10.8, of 8 20 and 10.8).
   if (R <= 4) {
     const dim3 grid((2 * H + FT / 32 - 1) / (FT / 32), static_cast<unsigned>(touched), B);
     if (bf) lantern_append_few_kernel<true><<<grid, FT, 0, st>>>(P);

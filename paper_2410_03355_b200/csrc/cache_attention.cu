@@ -32,11 +32,14 @@ lantern_status code_map(CUtensorMap* map, const void* code, const lantern_cache*
 }
 
 // Which kernel takes a call, and how its rows and tokens are divided.
-//   Up to 16 rows: `few` (128 single tokens of 4 heads a group over 2300 tokens: 112 us; as 64 rows mostly empty, 193).
+//   Up to 16 rows: `few` (128 single tokens of 4 heads a group over 2300 tokens: 116 us; as 64 rows mostly empty, 193).
 //   Up to 64 bf16 rows: `mid` where contexts are short, `wide` where they can be long enough for its units' longer start and end (trees of 61 rows, 20
-//   heads; 256 of 64 components over 650 tokens: mid 362 us, wide 400; 64 of them over 2250: 283 and 244; 64 of 128 components over 340 tokens: 138
-//   and 142, over 650: 197 and 181).  `room` is what the table can hold, about twice these averages.
-//   More rows, and fp32 ones from 17 on: `wide` (16 trees of 61 rows, 8 heads a group, 1200 tokens: 76 us, in 64 rows at a time as mid takes them 135).
+//   heads.  64 components: 64 trees over 140 tokens mid 49 us, wide 57; 256 over 640 363 and 363; 64 over 1120 155 and 143, over 2250 292 and 228.  128
+//   components: 64 over 140 89 and 107, over 340 133 and 129, over 640 196 and 169.  Where units are few `wide` is ahead on short contexts too: 2 trees
+//   over 140 tokens 15 and 13.5, 16 over 640 57 and 42).  A call knows no lengths: `room` is what the table can hold, about twice these averages where
+//   tables are cut to the contexts.  A wider table is taken for longer contexts: nothing for 256 trees over 640 tokens, and 9 to 11 us for one token, whose
+//   call then has a join that finds one part.
+//   More rows, and fp32 ones from 17 on: `wide` (16 trees of 61 rows, 8 heads a group, 1200 tokens: 73 us, in 64 rows at a time as mid takes them 135).
 static Division divide(int dtype, int B, int R, int q_heads, const lantern_cache* c, int width) {
   Division d;
   const int64_t G = q_heads / c->heads, M = G * R, room = static_cast<int64_t>(width) * c->page_tokens;

@@ -11,7 +11,8 @@ namespace lantern {
 // without a value.  So they are lifted towards a half's largest value, 2^16.  They refer to a maximum that follows the running one only when it
 // has fallen behind by 2^kLag, so that accumulators are rarely touched, and come with their value's scale over a largest one that may
 // have fallen behind by kScaleLag (few, mid), or with that scale's digits (wide, fp32): at most 2^4 * 2 * 2^10.  What is 2^-24 of the row's largest is still a normal half, what is lost is 2^-35 of
-// it.  A lag of 2^2 and 2^12 cost (256 trees; 16 trees of 8 heads a group by `wide`) 378 and 76.5 us, these 375 and 74.0; 2^8, 2^5 and no lift 368 and 74.0.
+// it.  A lag of 2^2 with 2^12 costs 0.5 % of 256 trees (mid) and 3.5 % of 16 trees of 8 heads a group (wide) more than these; 2^8, 2^5 and no lift 2 % less
+// and the same.
 constexpr float kLift = 1024.0f, kLag = 4.0f, kScaleLag = 2.0f;
 
 struct AttendParams {

@@ -11,7 +11,7 @@
 // lane's components of a token are 16 bytes side by side, a permutation of the products' inner axis), queries are halves after a power of two
 // of their own (8 bits of a bf16 query fit; an fp32 query goes in as two halves, 22 bits, and so do its probabilities).
 //
-// 128 single tokens, 32 heads over 8, contexts of 500 to 4100 tokens of 128 components: 112 us, 5.4 TB/s; with rows where products are 16 wide, a
+// 128 single tokens, 32 heads over 8, contexts of 500 to 4100 tokens of 128 components: 116 us, 5.2 TB/s; with rows where products are 16 wide, a
 // producer warp and barriers between four warps 193.
 #include "cache_attention.cuh"
 

@@ -9,7 +9,7 @@
 //
 // What costs is neither memory nor the tensor cores alone: ldmatrix (every warp reads the whole tile) and the products keep shared memory and the
 // tensor pipe half busy each, and a warp's chain from scores to output does the rest.  256 trees of 61 rows, 20 heads of 64 components over 650
-// tokens: 360 us (1.4 TB/s of codes); codes turned into halves by every warp for itself 505; 32 rows a warp 472 (registers).
+// tokens: 363 us (1.4 TB/s of codes); codes turned into halves by every warp for itself 505; 32 rows a warp 472 (registers).
 // Where contexts can be long the tcgen05 path takes the same rows (cache_attention_wide.cu; both sides of the line are measured at `divide`).
 #include "cache_attention.cuh"
 

@@ -19,7 +19,9 @@
 // its tiles.  What the other roles need to know of a tile travels with it.
 //
 // Bound by the softmax warps, one per scheduler and CTA, and by the instruction cache, which five roles' code shares: with all runs of tokens unrolled
-// 16 trees of 61 rows, 8 heads a group of 128 components over 1200 tokens took 102 us, in loops 76 (255 TFLOP/s).
+// 16 trees of 61 rows, 8 heads a group of 128 components over 1200 tokens took 102 us, in loops 73 (268 TFLOP/s).  At most 64
+// fp32 rows (one sequence of 32 over 100 000 tokens, 128 components: 61 us and 9 for the join) also keep the tensor pipe 46 % busy: their products are of 128
+// rows and two terms, a quarter of which counts.
 #include "cache_attention.cuh"
 
 namespace lantern {
