@@ -434,8 +434,9 @@ lantern_status lantern_cache_append(const void* k, const void* v, int dtype, int
  * EACH token up to 2^-35 of the row's largest probability, times its code under the largest value scale among the blocks that
  * the rows taken together see, is lost from the numerator (not from the sum).  n tokens that far behind one that has next to
  * no value of its own can so lose n * 2^-35 of that one's weight between them: 3e-6 for 100 000 tokens.  What of a value is
- * below 2^-32 of the largest value scale may be lost as well.  Value scales that are no powers of two (append leaves none)
- * are rounded to 11 bits on the way with bf16 rows, and not with fp32 ones.
+ * below 2^-32 of the largest value scale may be lost as well, and so may all of a block whose value scale is 2^-31 of the
+ * largest or less.  Value scales that are no powers of two (append leaves none) are rounded to 11 bits on the way with bf16
+ * rows, and not with fp32 ones.
  *
  *   q             [B, R, q_heads, D], strides in elements; 16-byte aligned rows are fastest, any alignment is served
  *   out           [B, R, q_heads, D] contiguous, dtype of q, 16-byte aligned; must not overlap q (out == q: LANTERN_E_PARAM)

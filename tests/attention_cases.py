@@ -39,7 +39,8 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
       lifted by 2^10, so that what lies below the smallest normal half loses 2^-25 * 2^-10 of the row's largest numerator, as a factor of a code under the largest
       value scale that the row's blocks have.
     * Values become halves times 2^7 over the largest scale: off by 2^-25 * 2^-7 of it (2 where a scale's own digits are put with the numerators), and with bf16,
-      where a scale is no power of two, by 2^-11 of themselves.
+      where a scale is no power of two, by 2^-11 of themselves.  The factor is a half itself, whose least is 2^-24: a block whose scale is below 2^-31 of the largest
+      (2^-30 where digits are put with the numerators) may be lost.
     * Sums.  The output adds up a product for each token whose value is not zero, one or two terms each, every addition off by 2^-23 of the magnitudes;
       accumulators and sums are scaled at most once per 32 tokens (2^-24); a sum takes at most a 32nd of its tokens one after the other, and what is put together
       of threads, warps and parts is below 64 additions more.
@@ -89,7 +90,7 @@ def attention(q, cache, table, lengths, counts=None, starts=None, parents=None, 
             err = (p * eps) @ v.abs() + (p * eps).sum(1, keepdim=True) * o.abs()
             err += (half + 2.0 ** -22 + (0.0 if f32 or exact else 2.0 ** -11)) * mag
             err += 2.0 ** -35 * vs[:, h].max() / total.clamp(min=1.0) * (mask.double() @ vcode)
-            err += 2.0 ** -31 * vs[:, h].max()
+            err += 2.0 ** -31 * vs[:, h].max() + p @ (v.abs() * (vs[:, h, None] < 2.0 ** -30 * vs[:, h].max()))
             err += (2 * terms * nonzero + count / 32 + 64) * 2.0 ** -23 * mag
             err += (count / 16 + 64) * 2.0 ** -24 * o.abs()
             out[b, :n, heads] = o.view(n, G, D)
