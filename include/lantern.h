@@ -460,7 +460,7 @@ lantern_status lantern_cache_attention(const void* q, void* out, int dtype, int 
  * scale, that block takes the larger one and its tokens are coded anew.
  * A fault (BAD_PATH, BAD_LENGTH, BAD_BLOCK) leaves the sequence as it is, with out_lengths[b] = lengths[b].
  *   accept_len    [B], accept_path [B, N] as lantern_verify writes them; B <= 65535, 0 <= N <= 1024
- *   out_lengths   [B], must not overlap lengths (out_lengths == lengths: LANTERN_E_PARAM) */
+ *   out_lengths   [B], must not overlap lengths, accept_len or accept_path (LANTERN_E_PARAM) */
 lantern_status lantern_cache_keep(const lantern_cache* cache, const int32_t* table, int table_width,
                                   const int32_t* lengths, const int32_t* accept_len, const int32_t* accept_path, int B,
                                   int N, int32_t* out_lengths, int32_t* status, void* cuda_stream);

@@ -608,7 +608,9 @@ extern "C" lantern_status lantern_cache_keep(const lantern_cache* cache, const i
   if (B < 0 || B > 65535 || N < 0 || N > 1024) return LANTERN_E_SHAPE;
   if (B == 0) return LANTERN_OK;
   if (!lengths || !accept_len || !out_lengths || (N > 0 && !accept_path)) return LANTERN_E_NULL;
-  if (out_lengths == lengths) return LANTERN_E_PARAM;
+  // (every warp of a sequence reads these, and one of them writes the new length)
+  const auto overlaps = [&](const int32_t* p, int64_t n) { return p && out_lengths < p + n && p < out_lengths + B; };
+  if (overlaps(lengths, B) || overlaps(accept_len, B) || overlaps(accept_path, static_cast<int64_t>(B) * N)) return LANTERN_E_PARAM;
   KeepParams P{view_of(cache, table, table_width), lengths, accept_len, accept_path, out_lengths, status, N};
   const dim3 grid((2 * cache->heads + KT / 32 - 1) / (KT / 32), B);
   lantern_keep_kernel<<<grid, KT, 0, static_cast<cudaStream_t>(cuda_stream)>>>(P);

@@ -111,6 +111,15 @@ def test_keep():
     assert keep(B=0) == 0
 
 
+def test_keep_results_in_place_of_inputs():
+    B, N = 4, 3
+    far = dict(B=B, N=N, lengths=AT, accept=AT + 4096, path=AT + 8192)
+    for at, size in ((AT, 4 * B), (AT + 4096, 4 * B), (AT + 8192, 4 * B * N)):
+        for out in (at, at + size - 4, at - 4 * B + 4):
+            assert keep(**far, out=out) == PARAM
+    assert keep(**{**far, "N": 0, "path": None}, out=AT) == PARAM
+
+
 def test_read():
     assert read(first=None) == NULL and read(k=None) == NULL and read(v=None) == NULL
     assert read(k=AT + 8) == ALIGN and read(B=1 << 16, R=1 << 16) == SHAPE
